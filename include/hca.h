@@ -574,6 +574,108 @@ int32_t hca_vq_evict(const hca_shape* shape, const hca_vq_codebook* cb, void* pc
                      const int64_t* n_resident, int64_t M, int64_t n_protect, int32_t* kept_opt, void* workspace,
                      void* pcache_dst, float* acc_dst, int32_t* pos_dst, void* stream);
 
+/* ---- Paged 8-bit cache: whole contexts attended -------------------------------------------------
+ * For the layers and requests that attend to everything (Eq. 1, no selection): prompts and chunks of prompts, short
+ * contexts, layers kept dense, a decoder's queries over an encoder's states.  Keys and values are held in pages of P
+ * tokens, 8 bits per number with one fp32 scale per page, KV head and side (keys, values).  A sequence is a row of the
+ * page table; a server keeps one row per request for the request's lifetime, idle rows have length 0.
+ *
+ * The block of a sequence that is not whole yet (its last length % P tokens) stays in 16 bits, as given, in the
+ * sequence's open rows; when its last token arrives the block is coded once:
+ *   amax  = largest magnitude of the block's P * head_dim numbers of one KV head and side
+ *   scale = max(fp32(amax / m), 2^-64), m = 127 (int8) or 448 (e4m3); inv = fp32(1 / scale)
+ *   code  = x * inv (fp32), clamped to [-m, m], rounded to nearest, ties to even
+ * so the codes do not depend on how a sequence was cut into calls, and no number is rounded twice.
+ *
+ * All lengths, tables and counts are device memory: nothing is read back, and calls can be captured and replayed while
+ * lengths change.  What a kernel reads from them is checked there: a page number outside [0, n_pages) holds no tokens
+ * (reads skip it, writes are dropped), row offsets are cut at the rows the call was given.
+ *   tables  int32 [n_seqs, max_pages]: page of each block of each sequence
+ *   kv      8-bit codes [n_pages, n_kv_heads, 2, P * head_dim]: keys, then values, in tiles of 16 tokens laid out
+ *           as the matrix core takes them (one 16-byte load per lane):
+ *             keys    [P/16][head_dim/64][4 g][16 t][16 e]      token t of the tile, channel 64 * second + 16 g + e
+ *             values  [P/16][head_dim/64][4 g][16 c][4 u][4 j]  token 4 g + j of the tile, channel 64 * second + 16 u + c
+ *   scale   fp32 [n_pages, n_kv_heads, 2]
+ *   open    elem [n_seqs, n_kv_heads, 2, P * head_dim]: rows in the same tiles
+ * kv, scale and open need no initial values; kv, open and rows of new keys, values and queries are 16-byte aligned.
+ * Supported: head_dim 64 or 128; page 16, 32, 64 or 128; n_q_heads / n_kv_heads 1 .. 16; up to 1024 sequences and 2^30
+ * tokens per sequence; n_pages * page below 2^31.  Anything else: HCA_ERR_UNSUPPORTED. */
+#define HCA_F16 0      /* elem: IEEE half */
+#define HCA_BF16 1     /* elem: bfloat16 */
+#define HCA_INT8 0     /* code: signed integers -127 .. 127 */
+#define HCA_E4M3 1     /* code: OCP 8-bit floats, 4 exponent and 3 mantissa bits */
+typedef struct {
+  int32_t n_seqs;      /* rows of the page table */
+  int32_t n_q_heads;
+  int32_t n_kv_heads;
+  int32_t head_dim;
+  int32_t page;        /* P */
+  int32_t max_pages;   /* blocks per sequence at most */
+  int32_t elem;        /* type of keys, values, queries, open rows and outputs */
+  int32_t code;        /* type of the codes in kv */
+  int64_t n_pages;     /* pages in kv */
+} hca_paged_shape;
+
+/* Bytes of the three buffers of one layer; 0 if the shape is unsupported. */
+size_t hca_paged_cache_bytes(const hca_paged_shape* shape);   /* kv */
+size_t hca_paged_scale_bytes(const hca_paged_shape* shape);   /* scale */
+size_t hca_paged_open_bytes(const hca_paged_shape* shape);    /* open */
+/* Workspace of hca_paged_attend for up to total_q query rows, max_q per sequence; 0 if the shape is unsupported. */
+size_t hca_paged_workspace_bytes(const hca_paged_shape* shape, int64_t total_q, int32_t max_q);
+
+/* One scheduling step of the page tables, before the layers store and attend (one call for all layers).
+ *   add        device, int32 [n_seqs]: new tokens of each sequence; negative: the sequence ends, all its pages go
+ *              back to the free list and its length becomes 0
+ *   lens_in, lens_out    device, int32 [n_seqs]: tokens before and after (may be the same array)
+ *   tables     device, updated: new pages are entered behind the ones in use; other entries stay
+ *   free_pages device, int32 [n_pages]: a stack of unused page numbers, updated
+ *   free_in, free_out    device, int32 [1]: how many of its entries count, before and after (may be the same)
+ *   max_new    rows of the new tokens' arrays
+ *   start      device, int32 [n_seqs]: position of the sequence's first new token; -1: refused, see below
+ *   cu         device, int32 [n_seqs + 1]: sequence b's new tokens are rows cu[b] .. cu[b+1] - 1 (running sums of
+ *              max(add, 0), cut at max_new)
+ *   tok_seq, tok_pos, tok_slot   device, int32 [max_new] each, or NULL: sequence, position and slot (page * P + position
+ *              % P) of every new token; -1 position and slot in a refused sequence; rows from cu[n_seqs] on are left
+ *              as they were
+ * Pages of ending sequences are pushed first (ascending sequence, ascending block), then pages are popped in the
+ * same order, so a step can use what it frees.  A sequence is refused - its length and pages stay as they were -
+ * if its length would pass max_pages * P, if its rows would pass max_new, or if it needs pages and the pages
+ * needed by it and the sequences before it (those refused for lack of pages included) are more than there are. */
+int32_t hca_paged_map(const hca_paged_shape* shape, const int32_t* add, const int32_t* lens_in, int32_t* lens_out,
+                      int32_t* tables, int32_t* free_pages, const int32_t* free_in, int32_t* free_out, int64_t max_new,
+                      int32_t* start, int32_t* cu, int32_t* tok_seq, int32_t* tok_pos, int32_t* tok_slot, void* stream);
+
+/* Appends one layer's new keys and values: blocks that become whole are coded into their pages, the rows of the block
+ * that stays open go to the open rows.
+ *   k, v       device, elem; row r, head h, channel c at r * stride + h * head_dim + c (strides in numbers, at least
+ *              n_kv_heads * head_dim and a multiple of 8: slices of a fused projection will do)
+ *   total      rows of k and v
+ *   start, cu  device, as hca_paged_map leaves them (start < 0: nothing of that sequence is stored)
+ * Open rows that hold no token of the open block keep what they held.  Two rows of the table must not share a page
+ * that the call writes. */
+int32_t hca_paged_store(const hca_paged_shape* shape, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                        int64_t total, const int32_t* start, const int32_t* cu, const int32_t* tables, void* kv,
+                        float* scale, void* open, void* stream);
+
+/* Softmax attention (Eq. 1) of every sequence's queries over its cached tokens: s = sm_scale * q . k, y = softmax(s) v,
+ * lse = log sum exp s, with k and v as the cache holds them (code * scale, open rows as they are).
+ *   q          device, elem; row r, head hq, channel c at r * q_stride + hq * head_dim + c (stride as above)
+ *   cu         device, int32 [n_seqs + 1]: sequence b's queries are rows cu[b] .. cu[b+1] - 1, in order of position
+ *   total_q    rows of q, y and lse; rows of no sequence are left as they were
+ *   max_q      no sequence has more queries than that (of one that has, only the first max_q rows are computed)
+ *   lens       device, int32 [n_seqs]: tokens in the cache, the queries' own among them if they were stored first
+ *   max_len    the longest of them as far as the caller knows; it chooses how the work is divided, any value is right
+ *   causal     != 0: the last query of a sequence stands at its last token, query i of m sees the tokens at positions
+ *              <= lens - m + i; 0: every query sees every token (cross attention)
+ *   y          device, elem [total_q, n_q_heads, head_dim]; 0 where a query sees no token
+ *   lse        device, fp32 [total_q, n_q_heads] or NULL; -inf where a query sees no token
+ *   workspace  device, hca_paged_workspace_bytes(shape, total_q, max_q)
+ * Results do not depend on anything but the inputs and the sizes (no atomics). */
+int32_t hca_paged_attend(const hca_paged_shape* shape, const void* q, int64_t q_stride, const int32_t* cu, int64_t total_q,
+                         int32_t max_q, const int32_t* lens, int64_t max_len, const int32_t* tables, const void* kv,
+                         const float* scale, const void* open, float sm_scale, int32_t causal, void* y, float* lse,
+                         void* workspace, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -35,6 +35,12 @@ class hca_layer(C.Structure):
                 ("vq_centroids", C.c_void_p), ("vq_lut", C.c_void_p)]
 
 
+class hca_paged_shape(C.Structure):
+    _fields_ = [("n_seqs", C.c_int32), ("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("page", C.c_int32), ("max_pages", C.c_int32), ("elem", C.c_int32), ("code", C.c_int32),
+                ("n_pages", C.c_int64)]
+
+
 PIPELINE_MAX_SEL = 64
 PIPELINE_MAX_PIPE = 8
 
@@ -151,6 +157,18 @@ def lib():
         L.hca_vq_evict.argtypes = [sp, cbp, vp, vp, vp, vp, i64, i64, vp, vp, vp, vp, vp, vp]
         L.hca_vq_attend_gathered.restype = i32
         L.hca_vq_attend_gathered.argtypes = [sp, cbp, vp, vp, vp, vp, i32, f32, vp, vp, vp, vp]
+        pp = C.POINTER(hca_paged_shape)
+        for name in ("hca_paged_cache_bytes", "hca_paged_scale_bytes", "hca_paged_open_bytes"):
+            getattr(L, name).restype = C.c_size_t
+            getattr(L, name).argtypes = [pp]
+        L.hca_paged_workspace_bytes.restype = C.c_size_t
+        L.hca_paged_workspace_bytes.argtypes = [pp, i64, i32]
+        L.hca_paged_map.restype = i32
+        L.hca_paged_map.argtypes = [pp, vp, vp, vp, vp, vp, vp, vp, i64, vp, vp, vp, vp, vp, vp]
+        L.hca_paged_store.restype = i32
+        L.hca_paged_store.argtypes = [pp, vp, i64, vp, i64, i64, vp, vp, vp, vp, vp, vp, vp]
+        L.hca_paged_attend.restype = i32
+        L.hca_paged_attend.argtypes = [pp, vp, i64, vp, i64, i32, vp, i64, vp, vp, vp, vp, f32, i32, vp, vp, vp, vp]
         _lib = L
     return _lib
 
@@ -425,3 +443,50 @@ def hca_host_weighted_sum(shape, vrow, count, k, w_f16, v_host, host_stride, y, 
     """All tensors are CPU tensors (pinned or not); blocks until y is written."""
     _check(lib().hca_host_weighted_sum(C.byref(shape), _ptr(vrow), _ptr(count), int(k), _ptr(w_f16), _ptr(v_host),
                                        int(host_stride), _ptr(y), int(n_threads)), "hca_host_weighted_sum")
+
+
+# ---- paged 8-bit cache ---------------------------------------------------------------------------
+
+ELEMS = {"f16": 0, "bf16": 1}
+CODES = {"int8": 0, "e4m3": 1}
+
+
+def make_paged_shape(n_seqs, n_q_heads, n_kv_heads, page, n_pages, max_pages, head_dim=128, elem="f16", code="int8"):
+    return hca_paged_shape(n_seqs, n_q_heads, n_kv_heads, head_dim, page, max_pages, ELEMS[elem], CODES[code], n_pages)
+
+
+def hca_paged_cache_bytes(shape):
+    return int(lib().hca_paged_cache_bytes(C.byref(shape)))
+
+
+def hca_paged_scale_bytes(shape):
+    return int(lib().hca_paged_scale_bytes(C.byref(shape)))
+
+
+def hca_paged_open_bytes(shape):
+    return int(lib().hca_paged_open_bytes(C.byref(shape)))
+
+
+def hca_paged_workspace_bytes(shape, total_q, max_q):
+    return int(lib().hca_paged_workspace_bytes(C.byref(shape), int(total_q), int(max_q)))
+
+
+def hca_paged_map(shape, add, lens_in, lens_out, tables, free_pages, free_in, free_out, max_new, start, cu, tok_seq=None,
+                  tok_pos=None, tok_slot=None, stream=None):
+    _check(lib().hca_paged_map(C.byref(shape), _ptr(add), _ptr(lens_in), _ptr(lens_out), _ptr(tables), _ptr(free_pages),
+                               _ptr(free_in), _ptr(free_out), int(max_new), _ptr(start), _ptr(cu), _ptr(tok_seq),
+                               _ptr(tok_pos), _ptr(tok_slot), _stream(stream)), "hca_paged_map")
+
+
+def hca_paged_store(shape, k, k_stride, v, v_stride, total, start, cu, tables, kv, scale, open, stream=None):
+    _check(lib().hca_paged_store(C.byref(shape), _ptr(k), int(k_stride), _ptr(v), int(v_stride), int(total), _ptr(start),
+                                 _ptr(cu), _ptr(tables), _ptr(kv), _ptr(scale), _ptr(open), _stream(stream)),
+           "hca_paged_store")
+
+
+def hca_paged_attend(shape, q, q_stride, cu, total_q, max_q, lens, max_len, tables, kv, scale, open, sm_scale, causal, y,
+                     lse=None, workspace=None, stream=None):
+    _check(lib().hca_paged_attend(C.byref(shape), _ptr(q), int(q_stride), _ptr(cu), int(total_q), int(max_q), _ptr(lens),
+                                  int(max_len), _ptr(tables), _ptr(kv), _ptr(scale), _ptr(open), float(sm_scale),
+                                  1 if causal else 0, _ptr(y), _ptr(lse), _ptr(workspace), _stream(stream)),
+           "hca_paged_attend")

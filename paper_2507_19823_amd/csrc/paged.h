@@ -1,0 +1,71 @@
+// Paged 8-bit cache: what its kernels share.  Layout and definitions stand in hca.h.
+#pragma once
+#include "hca_internal.h"
+
+namespace hca {
+
+constexpr int kPagedMaxSeqs = 1024;
+constexpr int kPagedMaxGqa = 16;
+
+struct PagedView {       // a checked hca_paged_shape
+  int32_t n_seqs, hq, hkv, gqa, D, P, lp, max_pages;   // lp = log2 P
+  int32_t elem, code;
+  int64_t n_pages;
+  __host__ __device__ int64_t page_bytes() const { return (int64_t)hkv * 2 * P * D; }
+  __host__ __device__ int64_t side() const { return (int64_t)P * D; }     // numbers of one head and side of a page
+};
+
+int32_t paged_view(const hca_paged_shape* s, PagedView* V);
+
+inline bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+
+#ifdef __HIPCC__
+// Place of (token t of the block, channel ch) in a block's keys and values.
+__device__ __forceinline__ int key_at(int t, int ch, int D) {
+  return (t >> 4) * (16 * D) + (ch >> 6) * 1024 + ((ch >> 4) & 3) * 256 + (t & 15) * 16 + (ch & 15);
+}
+__device__ __forceinline__ int value_at(int t, int ch, int D) {
+  return (t >> 4) * (16 * D) + (ch >> 6) * 1024 + ((t >> 2) & 3) * 256 + (ch & 15) * 16 + ((ch >> 4) & 3) * 4 + (t & 3);
+}
+
+template <bool BF16> __device__ __forceinline__ float elem_to_float(uint32_t bits16) {
+  return BF16 ? __uint_as_float(bits16 << 16) : h2f(bits16);
+}
+// round to nearest even; infinities and NaN stay what they are
+template <bool BF16> __device__ __forceinline__ uint16_t float_to_elem(float x) {
+  return BF16 ? __builtin_bit_cast(uint16_t, (__bf16)x) : f2h_bits(x);
+}
+
+// Rows of sequence b: [*first, *first + returned), cut at the `total` rows there are.
+__device__ __forceinline__ int paged_rows(const int32_t* __restrict__ cu, int b, int total, int* first) {
+  int lo = cu[b], hi = cu[b + 1];
+  lo = lo < 0 ? 0 : lo > total ? total : lo;
+  hi = hi < lo ? lo : hi > total ? total : hi;
+  *first = lo;
+  return hi - lo;
+}
+
+// Work items are numbered sequence by sequence; count(b) of them belong to sequence b.  Called by whole waves with a
+// uniform `item`: the sequence that holds it (n_seqs if there are fewer items) and the item's number inside it.  64
+// sequences per step by a DPP scan: one step for most batches, and no pass that would have to prepare a list.
+template <typename F>
+__device__ __forceinline__ int paged_find(int n_seqs, int item, int* within, F&& count) {
+  const int lane = threadIdx.x & 63;
+  int before = 0;
+  for (int b0 = 0; b0 < n_seqs; b0 += 64) {
+    const int c = b0 + lane < n_seqs ? count(b0 + lane) : 0;
+    const int incl = (int)wave_scan_incl((uint32_t)c);
+    const uint64_t past = __ballot(before + incl > item);
+    if (past != 0) {
+      const int l = __builtin_ctzll(past);
+      *within = item - before - (__builtin_amdgcn_readlane(incl, l) - __builtin_amdgcn_readlane(c, l));
+      return b0 + l;
+    }
+    before += (int)wave_last((uint32_t)incl);
+  }
+  *within = 0;
+  return n_seqs;
+}
+#endif
+
+}  // namespace hca

@@ -95,3 +95,51 @@ class LayerState:
         zero = torch.zeros(self.batch, self.hkv, self.cap, ng, dtype=torch.float16, device=self.device)
         B.hca_export_kcache(self.shape, self.kcache, self.n, codes, scale, zero)
         return codes, scale, zero
+
+
+class PagedCache:
+    """Page tables of n_seqs sequences and the paged 8-bit caches of n_layers layers behind them.
+
+    A step is: step() once, then store() and attend() per layer, all on one stream (they share a workspace and the
+    step's row offsets).  Nothing is read back from the device, so a captured step can be replayed with other lengths."""
+
+    def __init__(self, n_layers, n_seqs, n_q_heads, n_kv_heads, page, n_pages, max_pages, head_dim=128, elem="f16",
+                 code="e4m3", max_tokens=1, device="cuda"):
+        self.shape = B.make_paged_shape(n_seqs, n_q_heads, n_kv_heads, page, n_pages, max_pages, head_dim, elem, code)
+        nbytes = B.hca_paged_cache_bytes(self.shape)
+        if nbytes == 0:
+            raise B.HcaError("hca_paged_cache_bytes", -2)
+        i32 = dict(dtype=torch.int32, device=device)
+        self.dtype = {"f16": torch.float16, "bf16": torch.bfloat16}[elem]
+        self.max_tokens, self.max_len = max_tokens, max_pages * page
+        side = page * head_dim
+        self.kv = [torch.empty(n_pages, n_kv_heads, 2, side, dtype=torch.uint8, device=device) for _ in range(n_layers)]
+        self.scale = [torch.empty(n_pages, n_kv_heads, 2, device=device) for _ in range(n_layers)]
+        self.open = [torch.empty(n_seqs, n_kv_heads, 2, side, dtype=self.dtype, device=device) for _ in range(n_layers)]
+        self.tables = torch.full((n_seqs, max_pages), -1, **i32)
+        self.free = torch.arange(n_pages - 1, -1, -1, **i32)        # page 0 is given first
+        self.n_free = torch.full((1,), n_pages, **i32)
+        self.lens = torch.zeros(n_seqs, **i32)
+        self.start = torch.zeros(n_seqs, **i32)
+        self.cu = torch.zeros(n_seqs + 1, **i32)
+        self.tok = torch.full((3, max_tokens), -1, **i32)           # sequence, position, slot of each new token
+        self.ws = torch.empty(B.hca_paged_workspace_bytes(self.shape, max_tokens, max_tokens), dtype=torch.uint8, device=device)
+        self.sm_scale = 1.0 / math.sqrt(head_dim)
+
+    def step(self, add, total, stream=None):
+        """add: device int32 [n_seqs], new tokens per sequence, negative where one ends; total: rows that the step's keys,
+        values and queries have (>= the sum of the positive entries, <= max_tokens)."""
+        assert total <= self.max_tokens
+        B.hca_paged_map(self.shape, add, self.lens, self.lens, self.tables, self.free, self.n_free, self.n_free, total, self.start,
+                        self.cu, self.tok[0], self.tok[1], self.tok[2], stream)
+
+    def store(self, layer, k, v, stream=None):
+        """k, v: [total, n_kv_heads, head_dim], rows as step() numbered them; slices of a fused projection will do."""
+        B.hca_paged_store(self.shape, k, k.stride(0), v, v.stride(0), k.shape[0], self.start, self.cu, self.tables,
+                          self.kv[layer], self.scale[layer], self.open[layer], stream)
+
+    def attend(self, layer, q, max_q, y, lse=None, causal=True, max_len=None, cu=None, stream=None):
+        """q: [total, n_q_heads, head_dim] -> y, for the step's own tokens; cu: row offsets of other queries (cross attention)."""
+        B.hca_paged_attend(self.shape, q, q.stride(0), self.cu if cu is None else cu, q.shape[0], max_q, self.lens,
+                           self.max_len if max_len is None else max_len, self.tables, self.kv[layer], self.scale[layer],
+                           self.open[layer], self.sm_scale, causal, y, lse, self.ws, stream)

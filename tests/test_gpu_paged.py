@@ -1,0 +1,469 @@
+"""Paged 8-bit cache on the GPU against the plain definitions of paged_ref.py."""
+import math
+import random
+
+import pytest
+import torch
+
+import paged_ref as R
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def B():
+    if not torch.cuda.is_available():
+        pytest.skip("needs a GPU")
+    from paper_2507_19823_amd import binding
+    binding.lib()
+    return binding
+
+
+def dev(x, dtype=torch.int32):
+    return torch.tensor(x, dtype=dtype, device="cuda")
+
+
+# ---- page tables ---------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("n_seqs,page,n_pages,max_pages,new,seed", [
+    (1, 16, 40, 30, 200, 1), (5, 32, 23, 9, 60, 2), (64, 64, 300, 12, 150, 3), (70, 16, 5000, 64, 90, 4),
+    (300, 128, 400, 5, 300, 5), (1024, 16, 3000, 7, 60, 6), (3, 16, 3000, 2000, 9000, 7)])
+@pytest.mark.parametrize("alias", [False, True])
+def test_map_follows_the_rules_over_many_steps(B, n_seqs, page, n_pages, max_pages, new, seed, alias):
+    """Prompts, decode steps, endings, too few pages, tables that are full, rows past max_new."""
+    rng = random.Random(seed)
+    free = list(range(n_pages))
+    rng.shuffle(free)
+    ref = R.Tables(n_seqs, page, n_pages, max_pages, free)
+    shape = B.make_paged_shape(n_seqs, 1, 1, page, n_pages, max_pages)
+    tables = torch.full((n_seqs, max_pages), -1, dtype=torch.int32, device="cuda")
+    fr, cnt, lens = dev(free), dev([n_pages]), dev([0] * n_seqs)
+    start, cu = dev([0] * n_seqs), dev([0] * (n_seqs + 1))
+    refused = 0
+    for step in range(12):
+        add = [rng.choice([1, 1, 1, 0, -1, rng.randint(1, new), rng.randint(1, new)]) for _ in range(n_seqs)]
+        total = sum(max(a, 0) for a in add)
+        max_new = total if step % 3 else max(0, total - rng.randint(0, 5)) + (3 if step % 2 else 0)
+        tok = torch.full((3, max_new + 2), -9, dtype=torch.int32, device="cuda")
+        lens2, cnt2 = (lens, cnt) if alias else (torch.empty_like(lens), torch.empty_like(cnt))
+        print(f"map seqs={n_seqs} step={step} max_new={max_new}", flush=True)
+        B.hca_paged_map(shape, dev(add), lens, lens2, tables, fr, cnt, cnt2, max_new, start, cu, tok[0], tok[1], tok[2])
+        lens, cnt = lens2, cnt2
+        rs, rc, rt = ref.step(add, max_new)
+        refused += sum(s < 0 for s in rs)
+        assert start.tolist() == rs and cu.tolist() == rc
+        assert lens.tolist() == ref.lens and cnt.item() == ref.count
+        assert tables.tolist() == ref.tables
+        assert fr.tolist()[:ref.count] == ref.free[:ref.count]
+        want = torch.full((max_new + 2, 3), -9, dtype=torch.int32)
+        if rt:
+            want[:len(rt)] = torch.tensor(rt, dtype=torch.int32)
+        assert torch.equal(tok.cpu().T, want)
+    assert refused > 0          # the steps did reach the refusals
+
+
+def test_map_without_slot_arrays_and_without_tokens(B):
+    shape = B.make_paged_shape(2, 1, 1, 16, 4, 4)
+    tables, fr = torch.full((2, 4), -1, dtype=torch.int32, device="cuda"), dev([0, 1, 2, 3])
+    lens, cnt, start, cu = dev([0, 0]), dev([4]), dev([7, 7]), dev([7, 7, 7])
+    B.hca_paged_map(shape, dev([0, 0]), lens, lens, tables, fr, cnt, cnt, 0, start, cu)
+    assert start.tolist() == [0, 0] and cu.tolist() == [0, 0, 0] and cnt.item() == 4
+    B.hca_paged_map(shape, dev([17, 1]), lens, lens, tables, fr, cnt, cnt, 18, start, cu)
+    assert lens.tolist() == [17, 1] and tables.tolist() == [[3, 2, -1, -1], [1, -1, -1, -1]] and cnt.item() == 1
+
+
+# ---- store ---------------------------------------------------------------------------------------
+
+class Rig:
+    """A cache on the GPU and its plain counterpart, fed the same steps."""
+
+    def __init__(self, B, n_seqs, hq, hkv, D, P, elem, code, n_pages, max_pages, seed, poison=True):
+        self.B, self.n_seqs, self.hq, self.hkv, self.D, self.P, self.elem, self.code = B, n_seqs, hq, hkv, D, P, elem, code
+        self.n_pages, self.max_pages = n_pages, max_pages
+        self.g = torch.Generator().manual_seed(seed)
+        self.shape = B.make_paged_shape(n_seqs, hq, hkv, P, n_pages, max_pages, D, elem, code)
+        kv = torch.randint(0, 256, (n_pages, hkv, 2, P * D), generator=self.g, dtype=torch.uint8)
+        scale = torch.full((n_pages, hkv, 2), math.nan)
+        open_ = torch.full((n_seqs, hkv, 2, P * D), math.nan, dtype=R.ELEM[elem])    # no value of it may be used
+        if not poison:
+            kv.zero_(), scale.fill_(1.0), open_.zero_()
+        self.ref = R.Cache(n_seqs, hkv, P, n_pages, D, elem, code, kv, scale, open_)
+        self.kv, self.scale, self.open = kv.cuda(), scale.cuda(), open_.cuda()
+        order = torch.randperm(n_pages, generator=self.g).tolist()
+        self.tables = [order[b * max_pages:(b + 1) * max_pages] for b in range(n_seqs)]
+        self.lens = [0] * n_seqs
+
+    def rows(self, *shape):
+        x = torch.randn(*shape, generator=self.g)
+        x[..., 3] *= 9.0
+        return x.to(R.ELEM[self.elem])
+
+    def store(self, new, start=None, fused=False, k=None, v=None, extra=0):
+        cu = [0]
+        for t in new:
+            cu.append(cu[-1] + t)
+        start = list(self.lens) if start is None else start
+        total = cu[-1] + extra
+        if k is None:
+            k, v = self.rows(total, self.hkv, self.D), self.rows(total, self.hkv, self.D)
+        if fused:
+            x = torch.full((total, self.hq + 2 * self.hkv, self.D), 7.0, dtype=k.dtype, device="cuda")
+            kd, vd = x[:, self.hq:self.hq + self.hkv], x[:, self.hq + self.hkv:]
+            kd.copy_(k), vd.copy_(v)
+        else:
+            kd, vd = k.cuda(), v.cuda()
+        print(f"store new={new[:8]} D={self.D} P={self.P} {self.elem} {self.code}", flush=True)
+        self.B.hca_paged_store(self.shape, kd, kd.stride(0) if total else self.hkv * self.D, vd,
+                               vd.stride(0) if total else self.hkv * self.D, total, dev(start), dev(cu), dev(self.tables),
+                               self.kv, self.scale, self.open)
+        self.ref.store(start, cu, k, v, self.tables)
+        for b, s in enumerate(start):
+            if s >= 0 and new[b]:
+                self.lens[b] = s + new[b]
+
+    def check(self):
+        torch.cuda.synchronize()
+        assert torch.equal(self.kv.cpu(), self.ref.kv)
+        assert torch.equal(self.scale.cpu().view(torch.int32), self.ref.scale.view(torch.int32))
+        assert torch.equal(self.open.cpu().view(torch.int16), self.ref.open.view(torch.int16))
+
+    def attend(self, q, cu, max_q=None, causal=True, max_len=None, want=None, sm=None, pad=0, stream=None, ws=None):
+        """Runs the call on q [total, hq, D] and compares with the definition; returns (y, lse)."""
+        B, total = self.B, q.shape[0]
+        m = [b - a for a, b in zip(cu, cu[1:])]
+        max_q = max(m + [0]) if max_q is None else max_q
+        sm = 1.0 / math.sqrt(self.D) if sm is None else sm
+        qd = torch.full((total, self.hq * self.D + pad), 3.0, dtype=q.dtype, device="cuda")
+        qd[:, :self.hq * self.D] = q.reshape(total, -1)
+        y = torch.full((total, self.hq, self.D), -77.0, dtype=q.dtype, device="cuda")
+        lse = torch.full((total, self.hq), -77.0, device="cuda")
+        if ws is None:
+            ws = torch.full((B.hca_paged_workspace_bytes(self.shape, total, max_q),), 255, dtype=torch.uint8, device="cuda")
+        print(f"attend lens={self.lens[:8]} m={m[:8]} D={self.D} P={self.P} hq={self.hq}/{self.hkv} {self.elem} {self.code} "
+              f"causal={causal}", flush=True)
+        B.hca_paged_attend(self.shape, qd, qd.stride(0), dev(cu), total, max_q, dev(self.lens),
+                           max(self.lens) if max_len is None else max_len, dev(self.tables), self.kv, self.scale, self.open, sm,
+                           causal, y, lse, ws, stream)
+        torch.cuda.synchronize()
+        self.compare(q, cu, y, lse, causal, sm)
+        return y, lse
+
+    def compare(self, q, cu, y, lse, causal, sm):
+        y, lse = y.cpu(), lse.cpu()
+        assert bool((y[cu[-1]:] == -77.0).all()) and bool((lse[cu[-1]:] == -77.0).all())      # rows of no sequence
+        for b in range(self.n_seqs):
+            r0, r1 = cu[b], cu[b + 1]
+            k, v, there = self.ref.read(b, self.lens[b], self.tables)
+            ry, rl, mass, big = R.attend(q[r0:r1], k, v, there, sm, causal, self.hq // self.hkv)
+            ty, tl = R.tolerances(ry, rl, mass, big, self.lens[b], self.D, self.elem)
+            assert bool(((y[r0:r1].double() - ry).abs() <= ty).all()), (b, ((y[r0:r1].double() - ry).abs() / ty).max())
+            empty = torch.isinf(rl)
+            assert torch.equal(torch.isinf(lse[r0:r1]) & (lse[r0:r1] < 0), empty)
+            d = (lse[r0:r1].double() - rl)[~empty].abs()
+            assert bool((d <= tl[~empty]).all()), (b, d.max())
+
+
+@pytest.mark.parametrize("code", ["int8", "e4m3"])
+@pytest.mark.parametrize("D,P,elem", [(128, 64, "f16"), (128, 16, "bf16"), (64, 128, "bf16"), (64, 32, "f16"), (128, 128, "f16")])
+def test_store_in_steps_of_any_length(B, D, P, elem, code):
+    rig = Rig(B, 4, 6, 3, D, P, elem, code, 60, 12, seed=D + P)
+    for new in ([1, 0, P - 1, P], [1, 1, 1, 1], [P, 2 * P + 3, 1, 0], [0, 0, 0, 0], [3 * P - 2, P - 4, 2, P + 1], [1, 1, 0, 1]):
+        rig.store(new, fused=sum(new) % 2 == 0)
+        rig.check()
+
+
+def test_store_one_token_at_a_time_equals_one_call(B):
+    """The codes do not depend on how a sequence was cut into calls."""
+    a = Rig(B, 1, 2, 2, 128, 32, "bf16", "e4m3", 8, 8, seed=1)
+    b = Rig(B, 1, 2, 2, 128, 32, "bf16", "e4m3", 8, 8, seed=1)
+    k, v = a.rows(75, 2, 128), a.rows(75, 2, 128)
+    a.store([75], k=k, v=v)
+    for i in range(75):
+        b.store([1], k=k[i:i + 1], v=v[i:i + 1])
+    a.check(), b.check()
+    for p in a.tables[0][:2]:
+        assert torch.equal(a.kv[p], b.kv[p]) and torch.equal(a.scale[p], b.scale[p])
+
+
+def test_store_skips_refused_sequences_and_bad_pages(B):
+    rig = Rig(B, 4, 2, 2, 64, 16, "f16", "int8", 40, 5, seed=9)
+    rig.tables[1][1] = -1
+    rig.tables[2][0] = 40              # one past the last page
+    rig.tables[3][2] = -2 ** 31
+    rig.store([40, 40, 40, 60], start=[-1, 0, 0, 0], extra=5)
+    rig.check()
+    assert rig.lens[0] == 0
+
+
+@pytest.mark.parametrize("code", ["int8", "e4m3"])
+def test_store_of_zeros_ties_tiny_and_huge_numbers(B, code):
+    rig = Rig(B, 1, 5, 5, 64, 16, "bf16", code, 4, 2, seed=3)
+    k, v = rig.rows(16, 5, 64), rig.rows(16, 5, 64)
+    k[:, 0] = 0.0                       # the least scale, codes 0
+    k[:, 1] = k[:, 1] * 2.0 ** -80      # below the least scale
+    k[:, 2] = k[:, 2].sign() * 3.0e38
+    k[:, 3] = (torch.arange(16)[:, None] * 8.0 - 63.5 + torch.arange(64)[None] % 8).to(k.dtype)
+    k[0, 3, 0] = R.QMAX[code]           # scale 1: values half way between codes
+    v[:, 0], v[:, 3] = -0.0, k[:, 3] * 0.25
+    rig.store([16], k=k, v=v)
+    rig.check()
+    assert bool((rig.scale[rig.tables[0][0], 0] == 2.0 ** -64).all())
+
+
+# ---- attention -----------------------------------------------------------------------------------
+
+def filled(B, lens, hq, hkv, D, P, elem, code, seed, spare=0, **kw):
+    mp = max(1, max(-(-n // P) for n in lens)) + spare
+    rig = Rig(B, len(lens), hq, hkv, D, P, elem, code, mp * len(lens) + 3, mp, seed, **kw)
+    rig.store(list(lens))
+    return rig
+
+
+HEADS = [(1, 1), (4, 1), (6, 2), (8, 8), (14, 7), (16, 1), (10, 2), (24, 2)]
+
+
+@pytest.mark.parametrize("elem", ["f16", "bf16"])
+@pytest.mark.parametrize("code", ["int8", "e4m3"])
+@pytest.mark.parametrize("D,P", [(128, 16), (128, 64), (64, 32), (64, 128), (128, 128), (64, 16)])
+def test_attend_single_queries_at_all_odd_lengths(B, D, P, elem, code):
+    """Lengths around a page, a tile and zero; sequences with no query between those with one."""
+    lens = [0, 1, P - 1, P, P + 1, 2 * P, 15, 17, 3 * P + 5, 333, 64, 63]
+    hq, hkv = HEADS[(D + P + len(elem) + len(code)) % len(HEADS)]
+    rig = filled(B, lens, hq, hkv, D, P, elem, code, seed=P + D)
+    cu = [0]
+    for b in range(len(lens)):
+        cu.append(cu[-1] + (0 if b == 5 else 1))
+    rig.attend(rig.rows(cu[-1] + 2, hq, D), cu, pad=16)
+
+
+@pytest.mark.parametrize("hq,hkv", HEADS)
+@pytest.mark.parametrize("causal", [True, False])
+def test_attend_few_queries_of_every_head_layout(B, hq, hkv, causal):
+    lens, m = [70, 5, 129, 0, 1, 300], [3, 5, 1, 2, 4, 7]        # more queries than tokens: the first see nothing
+    rig = filled(B, lens, hq, hkv, 128, 32, "f16", "e4m3", seed=hq)
+    cu = [0]
+    for t in m:
+        cu.append(cu[-1] + t)
+    rig.attend(rig.rows(cu[-1], hq, 128), cu, causal=causal)
+
+
+@pytest.mark.parametrize("D,P,elem,code,hq,hkv", [(128, 64, "f16", "int8", 8, 2), (128, 16, "bf16", "e4m3", 4, 4),
+                                                  (64, 32, "bf16", "int8", 6, 1), (64, 128, "f16", "e4m3", 5, 5),
+                                                  (128, 128, "bf16", "e4m3", 14, 2)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_attend_prompts(B, D, P, elem, code, hq, hkv, causal):
+    """Whole prompts, a chunk behind cached tokens, a single query beside them, a sequence without any."""
+    lens, m = [200, 333, 90, 257, 0, 64], [200, 130, 1, 0, 0, 64]
+    rig = filled(B, lens, hq, hkv, D, P, elem, code, seed=D + P)
+    cu = [0]
+    for t in m:
+        cu.append(cu[-1] + t)
+    rig.attend(rig.rows(cu[-1] + 1, hq, D), cu, causal=causal, pad=8)
+
+
+@pytest.mark.parametrize("n,m,P,code,elem,max_len", [(5000, 1, 16, "int8", "f16", None), (9001, 1, 64, "e4m3", "bf16", None),
+                                                     (7000, 6, 32, "e4m3", "f16", None), (6010, 200, 128, "int8", "bf16", None),
+                                                     (5000, 1, 64, "e4m3", "f16", 10), (5000, 2, 64, "int8", "f16", 1 << 30),
+                                                     (4100, 33, 16, "e4m3", "bf16", 0)])
+def test_attend_long_contexts(B, n, m, P, code, elem, max_len):
+    """One long sequence beside short ones; the caller's idea of the longest may be wrong either way."""
+    rig = filled(B, [n, 40, 0, n // 3], 8, 2, 128, P, elem, code, seed=n)
+    cu = [0, m, m + 1, m + 2, 2 * m + 2]
+    rig.attend(rig.rows(cu[-1], 8, 128), cu, max_len=max_len)
+
+
+def test_attend_many_sequences(B):
+    lens = [(37 * i) % 211 for i in range(200)]
+    rig = filled(B, lens, 4, 2, 64, 16, "bf16", "int8", seed=2)
+    rig.attend(rig.rows(200, 4, 64), list(range(201)))
+
+
+def test_attend_weights_of_one_sharp_peak_and_of_a_flat_row(B):
+    """Scores far apart (all weight on one token, the running maximum moving late) and all equal."""
+    rig = filled(B, [700, 700], 4, 1, 128, 32, "f16", "e4m3", seed=4)
+    q = rig.rows(2, 4, 128)
+    q[0] *= 12.0
+    q[1] = 0.0
+    rig.attend(q, [0, 1, 2])
+    rig.attend(q, [0, 1, 2], sm=3.0)
+
+
+def test_attend_pages_of_very_different_scales(B):
+    """Blocks of tiny and of large values side by side, keys too: nothing is lost against the larger ones."""
+    n, P = 400, 16
+    rig = Rig(B, 1, 4, 2, 128, P, "bf16", "e4m3", 30, 25, seed=5)
+    k, v = rig.rows(n, 2, 128), rig.rows(n, 2, 128)
+    f = torch.tensor([2.0 ** (-(i // P) % 5 * 6) for i in range(n)])[:, None, None]
+    v = (v.float() * f * 16.0).to(v.dtype)
+    k = (k.float() * (1.0 + 3.0 * (f > 0.1))).to(k.dtype)
+    k[64:80], v[64:80] = 0.0, 0.0
+    rig.store([n], k=k, v=v)
+    rig.attend(rig.rows(1, 4, 128), [0, 1])
+
+
+def test_attend_skips_pages_that_do_not_exist(B):
+    rig = filled(B, [300, 100], 4, 2, 128, 32, "f16", "int8", seed=6)
+    rig.tables[0][2], rig.tables[0][5], rig.tables[1] = -1, rig.n_pages, [-7] * rig.max_pages
+    rig.attend(rig.rows(3, 4, 128), [0, 2, 3])
+    rig.attend(rig.rows(100, 4, 128), [0, 90, 100])
+    rig.lens[1] = 96                    # nothing but missing pages: an empty row
+    y, lse = rig.attend(rig.rows(2, 4, 128), [0, 1, 2])
+    assert bool((y[1] == 0).all()) and bool(torch.isinf(lse[1]).all())
+
+
+def test_attend_computes_no_more_queries_than_told(B):
+    rig = filled(B, [100, 90], 4, 2, 128, 16, "f16", "e4m3", seed=7)
+    q = rig.rows(9, 4, 128)
+    full, _ = rig.attend(q, [0, 5, 9])
+    y = torch.full_like(full, -77.0)
+    ws = torch.empty(B.hca_paged_workspace_bytes(rig.shape, 9, 2), dtype=torch.uint8, device="cuda")
+    B.hca_paged_attend(rig.shape, q.cuda(), 512, dev([0, 5, 9]), 9, 2, dev(rig.lens), 100, dev(rig.tables), rig.kv, rig.scale,
+                       rig.open, 1 / math.sqrt(128), True, y, None, ws)
+    torch.cuda.synchronize()
+    assert bool((y[2:5] == -77).all()) and bool((y[7:] == -77).all())
+    assert torch.allclose(y[[0, 1, 5, 6]].float(), full[[0, 1, 5, 6]].float(), rtol=2 ** -9, atol=2 ** -9)
+
+
+def test_attend_same_bits_every_time_and_on_another_stream(B):
+    rig = filled(B, [3000, 50, 1200], 8, 2, 128, 64, "bf16", "e4m3", seed=8)
+    q = rig.rows(7, 8, 128)
+    a = rig.attend(q, [0, 3, 4, 7])
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    b = rig.attend(q, [0, 3, 4, 7], stream=side)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+def test_attend_two_calls_at_once(B):
+    """Two streams, two workspaces, one cache."""
+    rig = filled(B, [9000, 4000], 8, 2, 128, 64, "f16", "int8", seed=10)
+    qs = [rig.rows(2, 8, 128), rig.rows(2, 8, 128)]
+    st = [torch.cuda.Stream(), torch.cuda.Stream()]
+    cu, lens, tables = dev([0, 1, 2]), dev(rig.lens), dev(rig.tables)
+    out = [(torch.zeros(2, 8, 128, dtype=torch.float16, device="cuda"), torch.zeros(2, 8, device="cuda"),
+            torch.empty(B.hca_paged_workspace_bytes(rig.shape, 2, 1), dtype=torch.uint8, device="cuda")) for _ in qs]
+    qd = [q.cuda() for q in qs]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for q, s, (y, lse, ws) in zip(qd, st, out):
+            B.hca_paged_attend(rig.shape, q, 1024, cu, 2, 1, lens, 9000, tables, rig.kv, rig.scale, rig.open, 1 / math.sqrt(128), True,
+                               y, lse, ws, s)
+    torch.cuda.synchronize()
+    for q, (y, lse, _) in zip(qs, out):
+        rig.compare(q, [0, 1, 2], y, lse, True, 1 / math.sqrt(128))
+
+
+# ---- together ------------------------------------------------------------------------------------
+
+def run_steps(cache, ref, tabs, steps, layers, hq, hkv, D, seed, step_call):
+    """Feeds `steps` (new tokens per sequence) to a PagedCache and to the plain definitions, comparing every output."""
+    g = torch.Generator().manual_seed(seed)
+    for add in steps:
+        total = sum(max(a, 0) for a in add)
+        qkv = torch.randn(layers, total, hq + 2 * hkv, D, generator=g).to(cache.dtype)
+        ys, lses = step_call(add, total, qkv)
+        start, cu, _ = tabs.step(add, total)
+        assert cache.lens.tolist() == tabs.lens and cache.start.tolist() == start
+        for layer in range(layers):
+            r = ref[layer]
+            r.store(start, cu, qkv[layer][:, hq:hq + hkv], qkv[layer][:, hq + hkv:], tabs.tables)
+            for b, s in enumerate(start):
+                if s < 0 or cu[b + 1] == cu[b]:
+                    continue
+                k, v, there = r.read(b, tabs.lens[b], tabs.tables)
+                ry, rl, mass, big = R.attend(qkv[layer][cu[b]:cu[b + 1], :hq], k, v, there, cache.sm_scale, True, hq // hkv)
+                ty, tl = R.tolerances(ry, rl, mass, big, tabs.lens[b], D, "bf16" if cache.dtype == torch.bfloat16 else "f16")
+                assert bool(((ys[layer][cu[b]:cu[b + 1]].cpu().double() - ry).abs() <= ty).all()), (add, layer, b)
+                assert bool(((lses[layer][cu[b]:cu[b + 1]].cpu().double() - rl).abs() <= tl).all())
+
+
+def make_pair(layers, n_seqs, hq, hkv, D, P, elem, code, n_pages, max_pages, max_tokens):
+    from paper_2507_19823_amd.session import PagedCache
+    c = PagedCache(layers, n_seqs, hq, hkv, P, n_pages, max_pages, D, elem, code, max_tokens)
+    ref = [R.Cache(n_seqs, hkv, P, n_pages, D, elem, code, c.kv[i].cpu(), c.scale[i].cpu(), c.open[i].cpu()) for i in range(layers)]
+    return c, ref, R.Tables(n_seqs, P, n_pages, max_pages, c.free.tolist())
+
+
+def test_requests_served_from_prompt_to_end(B):
+    """Prompts, decode steps beside a prompt's chunk, drafts, an ending request whose pages the next one takes, a request
+    refused for lack of pages: tables, store and attention of two layers as a server calls them."""
+    layers, hq, hkv, D = 2, 8, 2, 128
+    c, ref, tabs = make_pair(layers, 5, hq, hkv, D, 32, "bf16", "e4m3", 30, 20, 600)
+
+    def call(add, total, qkv):
+        x = qkv.cuda()
+        c.step(dev(add), total)
+        out = []
+        for i in range(layers):
+            c.store(i, x[i][:, hq:hq + hkv], x[i][:, hq + hkv:])
+            y, lse = torch.zeros(total, hq, D, dtype=c.dtype, device="cuda"), torch.zeros(total, hq, device="cuda")
+            c.attend(i, x[i][:, :hq], max(add + [1]), y, lse)
+            out.append((y, lse))
+        torch.cuda.synchronize()
+        return [o[0] for o in out], [o[1] for o in out]
+
+    steps = [[100, 37, 0, 0, 0], [1, 1, 250, 0, 0], [1, 1, 130, 5, 0], [4, 1, 3, 1, 0], [1, -1, 1, 1, 0], [1, 0, 1, 1, 400],
+             [1, 40, 1, 1, 90], [-1, 1, -1, 1, 300], [1, 1, 1, 1, 1]]
+    run_steps(c, ref, tabs, steps, layers, hq, hkv, D, 11, call)
+    assert tabs.lens[4] < 400 + 90 + 300          # not every request was granted
+
+
+def test_captured_step_replayed_while_lengths_grow(B):
+    """One decode step captured once and replayed: blocks become whole, sequences end and start between replays, and other
+    work runs between them.  A second graph with the same buffers runs in turn with the first."""
+    layers, hq, hkv, D, n = 1, 4, 2, 64, 3
+    c, ref, tabs = make_pair(layers, n, hq, hkv, D, 16, "f16", "int8", 20, 12, 64)
+    x = torch.zeros(n, hq + 2 * hkv, D, dtype=c.dtype, device="cuda")
+    add = dev([1] * n)
+    y, lse = torch.zeros(n, hq, D, dtype=c.dtype, device="cuda"), torch.zeros(n, hq, device="cuda")
+
+    def one():
+        c.step(add, n)
+        c.store(0, x[:, hq:hq + hkv], x[:, hq + hkv:])
+        c.attend(0, x[:, :hq], 1, y, lse)
+
+    graphs = []
+    for _ in range(2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            one()
+        graphs.append(g)
+    turn = [0]
+
+    def call(a, total, qkv):
+        add.copy_(dev(a))
+        x.zero_()
+        x[:total].copy_(qkv[0])
+        graphs[turn[0] % 2].replay()
+        turn[0] += 1
+        torch.cuda.synchronize()
+        _ = (x.float().sum() + 1).item()                  # the program's own work between replays
+        return [y[:total]], [lse[:total]]
+
+    steps = [[1, 1, 1]] * 15 + [[1, 0, 1], [1, 1, 1], [1, -1, 1], [1, 1, -1], [1, 1, 1]] + [[1, 1, 1]] * 14
+    run_steps(c, ref, tabs, steps, layers, hq, hkv, D, 12, call)
+
+
+def test_queries_over_an_encoders_states(B):
+    """Cross attention: the states are stored once, the decoder's queries have another length and no mask."""
+    hq, hkv, D = 6, 6, 64
+    c, ref, tabs = make_pair(1, 2, hq, hkv, D, 32, "f16", "e4m3", 20, 8, 300)
+    g = torch.Generator().manual_seed(3)
+    kv = torch.randn(250, 2, hkv, D, generator=g).half()
+    c.step(dev([150, 100]), 250)
+    c.store(0, kv.cuda()[:, 0], kv.cuda()[:, 1])
+    start, cu, _ = tabs.step([150, 100], 250)
+    ref[0].store(start, cu, kv[:, 0], kv[:, 1], tabs.tables)
+    for m in ([1, 1], [37, 200], [0, 5]):
+        q = torch.randn(sum(m), hq, D, generator=g).half()
+        y, lse = torch.zeros(sum(m), hq, D, dtype=torch.float16, device="cuda"), torch.zeros(sum(m), hq, device="cuda")
+        c.attend(0, q.cuda(), max(m), y, lse, causal=False, cu=dev([0, m[0], sum(m)]))
+        torch.cuda.synchronize()
+        at = 0
+        for b in range(2):
+            k, v, there = ref[0].read(b, tabs.lens[b], tabs.tables)
+            ry, rl, mass, big = R.attend(q[at:at + m[b]], k, v, there, c.sm_scale, False, 1)
+            ty, tl = R.tolerances(ry, rl, mass, big, tabs.lens[b], D, "f16")
+            assert bool(((y[at:at + m[b]].cpu().double() - ry).abs() <= ty).all())
+            assert bool(((lse[at:at + m[b]].cpu().double() - rl).abs() <= tl).all())
+            at += m[b]
