@@ -134,6 +134,7 @@ def attend(q, k, v, there, sm, causal, G):
     i = torch.arange(m)[:, None]
     hidden = ~there[None].expand(m, n) | ((torch.arange(n)[None] > n - m + i) if causal else torch.zeros(m, n, dtype=torch.bool))
     y = torch.zeros(m, hq, D, dtype=torch.float64)
+    # mass: sum p |v|, and the share of it that tolerances() gives to weights far below the largest
     mass = torch.zeros_like(y)
     lse = torch.full((m, hq), -math.inf, dtype=torch.float64)
     big = torch.zeros(m, hq, dtype=torch.float64)
@@ -149,14 +150,22 @@ def attend(q, k, v, there, sm, causal, G):
         y[:, h] = p @ v[h // G]
         mass[:, h] = p @ v[h // G].abs()
         big[:, h] = (q[:, h].abs() @ k[h // G].abs().T * sm).amax(1)
-    return y, lse, mass, big
+    return y, lse, mass + ABSOLUTE * n * v.abs().amax((1, 2)).repeat_interleave(G)[None, :, None], big
+
+
+# Weights are held in halves, p times the scale of the token's page relative to the largest such product, which stands
+# at 2^12 or above; halves below 2^-14 are 2^-24 apart, so a weight is off by at most 2^-25 / 2^12 of the largest, whatever its own
+# size.  A token adds that times its code, and the largest scale times the largest code is the largest |v| of the
+# head (m steps of the scale; an open block is scaled to the same range): 2^-37 n max|v| in all, taken twice.  The
+# bound on y multiplies its mass by rel >= 2^-11, so it is added there as 2^-36 / 2^-11.
+ABSOLUTE = 2.0 ** -25
 
 
 def tolerances(y, lse, mass, big, n, D, elem):
     """Bounds on the error of y and lse, by the arithmetic's roundings:
     a score is a sum of D exact products in 32 bits, then two multiplications and an addition: ds <= (D + 4) 2^-24 big;
     a weight carries exp(2 ds) of that, 2^-22 of the power's own error, and its rounding to 16 bits, 2^-11;
-    sums of n weights in 32 bits: n 2^-24 (the worst order); weights below 2^-39 of the largest may be lost: n 2^-38;
+    sums of n weights in 32 bits: n 2^-24 (the worst order); small weights: see ABSOLUTE;
     the result is rounded to its type once."""
     ds = (D + 4) * 2.0 ** -24 * big
     rel = 2 * ds + 2.0 ** -11 + 2.0 ** -21 + n * 2.0 ** -23
