@@ -108,7 +108,7 @@ struct Partial {          // of one item, KV head and row: reference, sum; the w
 };
 
 template <int D, int NT, bool E4M3>
-__global__ __launch_bounds__(256) void paged_rows_kernel(PagedView V, AttendArgs a, SplitPlan sp, Partial* __restrict__ ml,
+__global__ __launch_bounds__(256, NT == 1 ? 2 : 1) void paged_rows_kernel(PagedView V, AttendArgs a, SplitPlan sp, Partial* __restrict__ ml,
                                                          float* __restrict__ part) {
   constexpr int NH = D / 64, NC = D / 16, COLS = 16 * NT;
   extern __shared__ float lds[];                       // [4][COLS][D + 4], then M and l of each wave [4][COLS]
@@ -535,130 +535,335 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedView V, AttendArgs
   if (ch == 0 && a.lse != nullptr) a.lse[out] = sum > 0.f ? (M + log2f(sum)) * 0.693147180559945309f : -INFINITY;
 }
 
-template <bool E4M3> __device__ __forceinline__ void code_to_float(uint32_t w, float* x) {
-  if (E4M3) {
-    const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false);
-    const auto hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
-    x[0] = lo[0]; x[1] = lo[1]; x[2] = hi[0]; x[3] = hi[1];
-  } else {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = (float)(int)(int8_t)(w >> (8 * i));
-  }
+// ---- many query rows: the matrix cores are the bound -------------------------------------------------
+// A workgroup takes 32 query rows per wave (queries x heads of one KV head, the same columns of S^T = K Q^T and Y^T = V^T P^T
+// as above, in 32 x 32 products) and walks over the tokens in units of 64.  A unit's codes are converted once per
+// workgroup: wave w loads tile w of the unit (a tile lies in one page, or is open rows, or holds nothing), writes halves to
+// LDS in the order in which the products take them, 16 bytes per lane and no bank twice, while the waves work on the unit
+// before.  One barrier per unit.  Weights never leave their lane.
+typedef float f16v __attribute__((ext_vector_type(16)));
+
+__device__ __forceinline__ float halves_max(float x) {
+  const uint32_t xi = __float_as_uint(x);
+  const auto r = __builtin_amdgcn_permlane32_swap(xi, xi, false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float halves_sum(float x) {
+  const uint32_t xi = __float_as_uint(x);
+  const auto r = __builtin_amdgcn_permlane32_swap(xi, xi, false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-// One workgroup per query row and head; its four waves take tiles of 16 tokens in turn and their partial results
-// (running maximum, sum, weighted values) are joined in LDS.
-template <int D, bool BF16, bool E4M3>
-__global__ __launch_bounds__(256) void paged_attend_kernel(PagedView V, AttendArgs a) {
-  constexpr int NH = D / 64;
-  __shared__ float s_m[4], s_l[4], s_y[4][D];
-  const int hq = blockIdx.y, h = hq / V.gqa, lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const int l16 = lane & 15, g = lane >> 4;
-  int i;
-  const int b = paged_find(V.n_seqs, blockIdx.x, &i, [&](int s) { int f; return paged_rows(a.cu, s, a.total, &f); });
+// rows of sequence b (queries x heads of a KV head)
+__device__ __forceinline__ int seq_rows(const PagedView& V, const AttendArgs& a, int b) {
+  int f;
+  const int m = paged_rows(a.cu, b, a.total, &f);
+  return (m < a.max_q ? m : a.max_q) * V.gqa;
+}
+
+template <int D, bool E4M3>
+__global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedView V, AttendArgs a) {
+  constexpr int NH = D / 64, NS = D / 16, NC = D / 32, NW = 4, ROWS = 32 * NW;
+  extern __shared__ char lds_raw[];
+  h8* sk = reinterpret_cast<h8*>(lds_raw);                       // [2][D / 8][64]: 8 channels of a token
+  h8* sv = sk + 2 * (D / 8) * 64;                                // [2][4][2][D]: 8 tokens of a channel
+  float* sinfo = reinterpret_cast<float*>(sv + 2 * 8 * D);       // [2][4][4]: key scale, log2 and inverse of value scale
+  const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4, l32 = lane & 31, hh = lane >> 5;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int h = blockIdx.x % V.hkv;
+  int within;
+  const int b = paged_find(V.n_seqs, blockIdx.x / V.hkv, &within, [&](int s) { return (seq_rows(V, a, s) + ROWS - 1) / ROWS; });
   if (b >= V.n_seqs) return;
   int row0;
-  const int m = paged_rows(a.cu, b, a.total, &row0);
-  if (i >= a.max_q) return;
-  int n = a.lens[b];
-  n = n < 0 ? 0 : n > (V.max_pages << V.lp) ? V.max_pages << V.lp : n;
-  const int sees = a.causal ? (n - m + i + 1 < 0 ? 0 : n - m + i + 1) : n;
-  const uint16_t* qp = a.q + (int64_t)(row0 + i) * a.q_stride + (int64_t)hq * D;
-  float q[NH][16];
+  const int m_all = paged_rows(a.cu, b, a.total, &row0);
+  const int G = V.gqa, R = seq_rows(V, a, b);
+  const int rt = (R + ROWS - 1) / ROWS - 1 - within;             // the tiles that see most come first
+  const int n = seq_len(V, a, b), whole = n >> V.lp << V.lp;
+  const int64_t side = V.side();
+
+  // this lane's query row
+  const int r = rt * ROWS + 32 * w + l32;
+  const bool live = r < R;
+  const int qi = live ? r / G : (R - 1) / G, hq = h * G + (live ? r % G : 0);
+  const auto seen = [&](int i) {
+    const int s = n - m_all + i + 1;
+    return !a.causal ? n : s < 0 ? 0 : s;
+  };
+  const int sees = seen(qi);
+  h8 q[NS];
+  float qs = a.sm;
+  {
+    const uint16_t* qp = a.q + (int64_t)(row0 + qi) * a.q_stride + (int64_t)hq * D;
+    uint4 raw[NS];
+    float amax = 0.f;
 #pragma unroll
-  for (int x = 0; x < NH; ++x)
+    for (int s = 0; s < NS; ++s) {
+      raw[s] = live ? *reinterpret_cast<const uint4*>(qp + 16 * s + 8 * hh) : uint4{0, 0, 0, 0};
 #pragma unroll
-    for (int e = 0; e < 16; ++e) q[x][e] = elem_to_float<BF16>(qp[64 * x + 16 * g + e]);
-  float top = -1e30f, sum = 0.f, y[NH][4];
+      for (int i = 0; i < 4; ++i)
+        amax = fmaxf(amax, fmaxf(fabsf(elem_to_float<true>(word(raw[s], i) & 0xffffu)), fabsf(elem_to_float<true>(word(raw[s], i) >> 16))));
+    }
+    if (V.elem == HCA_BF16) {
+      amax = halves_max(amax);
+      int ex = amax > 0.f ? 14 - ilogbf(amax) : 0;
+      ex = ex > 100 ? 100 : ex;
+      const float up = ldexpf(1.0f, ex);
+      qs = ldexpf(a.sm, -ex);
 #pragma unroll
-  for (int x = 0; x < NH; ++x)
+      for (int s = 0; s < NS; ++s)
 #pragma unroll
-    for (int u = 0; u < 4; ++u) y[x][u] = 0.f;
-  const int whole = n >> V.lp << V.lp;              // tokens from here on are open rows
-  for (int t0 = w * 16; t0 < sees; t0 += 64) {
-    float k[NH][16], v[NH][16], ks = 1.f, vs = 1.f;
-    if (t0 < whole) {
-      const int page = a.tables[(int64_t)b * V.max_pages + (t0 >> V.lp)];
-      if (page < 0 || page >= V.n_pages) continue;
-      const int64_t at = ((int64_t)page * V.hkv + h) * 2;
-      const uint4* kp = reinterpret_cast<const uint4*>(a.kv + at * V.side() + (t0 & (V.P - 1)) * D);
-      const uint4* vp = reinterpret_cast<const uint4*>(a.kv + (at + 1) * V.side() + (t0 & (V.P - 1)) * D);
-      ks = a.scale[at];
-      vs = a.scale[at + 1];
-#pragma unroll
-      for (int x = 0; x < NH; ++x) {
-        const uint4 kw = kp[x * 64 + lane], vw = vp[x * 64 + lane];
-        const uint32_t kk[4] = {kw.x, kw.y, kw.z, kw.w}, vv[4] = {vw.x, vw.y, vw.z, vw.w};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          code_to_float<E4M3>(kk[e], &k[x][4 * e]);
-          code_to_float<E4M3>(vv[e], &v[x][4 * e]);
+        for (int i = 0; i < 4; ++i) {
+          q[s][2 * i] = (_Float16)(elem_to_float<true>(word(raw[s], i) & 0xffffu) * up);
+          q[s][2 * i + 1] = (_Float16)(elem_to_float<true>(word(raw[s], i) >> 16) * up);
         }
-      }
     } else {
-      const uint16_t* kp = a.open + ((int64_t)b * V.hkv + h) * 2 * V.side() + (t0 & (V.P - 1)) * D;
-      const uint16_t* vp = kp + V.side();
 #pragma unroll
-      for (int x = 0; x < NH; ++x)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          k[x][e] = elem_to_float<BF16>(kp[(x * 64 + lane) * 16 + e]);
-          const bool live = t0 + 4 * g + (e & 3) < n;          // rows behind the last token may hold anything
-          v[x][e] = live ? elem_to_float<BF16>(vp[(x * 64 + lane) * 16 + e]) : 0.f;
-        }
+      for (int s = 0; s < NS; ++s) q[s] = __builtin_bit_cast(h8, raw[s]);
     }
-    float s = 0.f;
+  }
+  const int least_seen = (int)wave_min((uint32_t)sees), most_seen = (int)wave_max((uint32_t)sees);
+  const int r_last = rt * ROWS + ROWS - 1 < R ? rt * ROWS + ROWS - 1 : R - 1;
+  const int units = (seen(r_last / G) + kUnit - 1) / kUnit;      // of the workgroup
+
+  float M = -1e30f, l = 0.f;
+  f16v y[NC];
 #pragma unroll
-    for (int x = 0; x < NH; ++x)
+  for (int c = 0; c < NC; ++c)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) s = fmaf(q[x][e], k[x][e], s);
-    s += __shfl_xor(s, 16);
-    s += __shfl_xor(s, 32);                                      // token l16's score on every lane row
-    s = t0 + l16 < sees ? s * (ks * a.sm) : -INFINITY;
-    float mx = s;
-#pragma unroll
-    for (int d = 1; d < 16; d <<= 1) mx = fmaxf(mx, __shfl_xor(mx, d));
-    const float nt = fmaxf(top, mx), f = exp2f(top - nt);
-    top = nt;
-    float p = exp2f(s - nt);
-    float ps = p;
-#pragma unroll
-    for (int d = 1; d < 16; d <<= 1) ps += __shfl_xor(ps, d);
-    sum = sum * f + ps;
-    p *= vs;
-    float pt[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) pt[j] = __shfl(p, 4 * g + j);
-#pragma unroll
-    for (int x = 0; x < NH; ++x)
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        y[x][u] *= f;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) y[x][u] = fmaf(pt[j], v[x][4 * u + j], y[x][u]);
+    for (int i = 0; i < 16; ++i) y[c][i] = 0.f;
+
+  // lane j holds the page of this wave's tile of unit base + j, and its scales
+  const int32_t* table = a.tables + (int64_t)b * V.max_pages;
+  struct Info { int id; float ks, vs; };
+  const auto fetch = [&](int base) {
+    const int t = (base + lane) * kUnit + 16 * w;
+    Info f{-1, 0.f, 1.f};
+    if (t < whole && base + lane < units) {
+      const int id = table[t >> V.lp];
+      if (id >= 0 && id < V.n_pages) {
+        const float2 sc = *reinterpret_cast<const float2*>(a.scale + ((int64_t)id * V.hkv + h) * 2);
+        f = Info{id, sc.x, sc.y};
       }
-  }
-#pragma unroll
-  for (int x = 0; x < NH; ++x)
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      y[x][u] += __shfl_xor(y[x][u], 16);
-      y[x][u] += __shfl_xor(y[x][u], 32);
-      if (g == 0) s_y[w][64 * x + 16 * u + l16] = y[x][u];
     }
-  if (lane == 0) { s_m[w] = top; s_l[w] = sum; }
-  __syncthreads();
-  const float all = fmaxf(fmaxf(s_m[0], s_m[1]), fmaxf(s_m[2], s_m[3]));
-  float l = 0.f, out = 0.f;
+    return f;
+  };
+  Info pages = fetch(0);
+  uint4 kw[NH], vw[NH];
+  float nks = 0.f, nvs = 1.f;
+  int nid = -1;
+  const auto load = [&](int u) {                                 // asks for the codes of this wave's tile of unit u
+    if ((u & 63) == 0 && u > 0) pages = fetch(u);
+    nid = __builtin_amdgcn_readlane(pages.id, u & 63);
+    nks = lane_value(pages.ks, u & 63);
+    nvs = lane_value(pages.vs, u & 63);
+    if (nid >= 0) {
+      const int t = u * kUnit + 16 * w;
+      const uint8_t* p = a.kv + ((int64_t)nid * V.hkv + h) * 2 * side + (t & (V.P - 1)) * D;
 #pragma unroll
-  for (int x = 0; x < 4; ++x) {
-    const float f = exp2f(s_m[x] - all);
-    l = fmaf(s_l[x], f, l);
-    if (threadIdx.x < D) out = fmaf(s_y[x][threadIdx.x], f, out);
+      for (int z = 0; z < NH; ++z) {
+        kw[z] = reinterpret_cast<const uint4*>(p)[z * 64 + lane];
+        vw[z] = reinterpret_cast<const uint4*>(p + side)[z * 64 + lane];
+      }
+    }
+  };
+  const auto put_key = [&](int buf, int z, int e, h8 x) { sk[(buf * (D / 8) + 8 * z + 2 * g + e) * 64 + 16 * w + l16] = x; };
+  const auto put_value = [&](int buf, int z, int u, h2 x0, h2 x1) {
+    uint2 o{__builtin_bit_cast(uint32_t, x0), __builtin_bit_cast(uint32_t, x1)};
+    *(reinterpret_cast<uint2*>(sv + ((buf * 4 + w) * 2 + (g & 1)) * D + 64 * z + 16 * u + l16) + (g >> 1)) = o;
+  };
+  const auto stage = [&](int u, int buf) {                       // ... and puts them into LDS as halves
+    const int t = u * kUnit + 16 * w;
+    float ks = nks, lv, iv;
+    if (nid >= 0) {
+      lv = log2_raw(nvs);
+      iv = 1.0f / nvs;
+#pragma unroll
+      for (int z = 0; z < NH; ++z)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) put_key(buf, z, e, codes_to_halves<E4M3>(word(kw[z], 2 * e), word(kw[z], 2 * e + 1)));
+#pragma unroll
+      for (int z = 0; z < NH; ++z)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          h2 o[2];
+          code_to_half<E4M3>(word(vw[z], x), o);
+          put_value(buf, z, x, o[0], o[1]);
+        }
+    } else if (t >= whole && t < n) {                            // open rows: scaled by powers of two, as above
+      const uint16_t* kp = a.open + ((int64_t)b * V.hkv + h) * 2 * side + (t & (V.P - 1)) * D;
+      int ex[2];
+#pragma unroll
+      for (int sd = 0; sd < 2; ++sd) {
+        uint4 raw[NH][2];
+        float amax = 0.f;
+        const auto widen = [&](uint32_t bits) { return V.elem == HCA_BF16 ? elem_to_float<true>(bits) : elem_to_float<false>(bits); };
+#pragma unroll
+        for (int z = 0; z < NH; ++z)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const uint4 v = *(reinterpret_cast<const uint4*>(kp + sd * side + (z * 64 + lane) * 16) + e);
+            uint32_t wd[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int a0 = sd == 0 ? t + l16 : t + 4 * g + 2 * (i & 1), a1 = sd == 0 ? t + l16 : a0 + 1;
+              wd[i] = (a0 < n ? wd[i] & 0xffffu : 0u) | (a1 < n ? wd[i] & 0xffff0000u : 0u);
+              amax = fmaxf(amax, fmaxf(fabsf(widen(wd[i] & 0xffffu)), fabsf(widen(wd[i] >> 16))));
+            }
+            raw[z][e] = uint4{wd[0], wd[1], wd[2], wd[3]};
+          }
+        amax = wave_max(amax);
+        ex[sd] = amax > 0.f && (sd == 1 || V.elem == HCA_BF16) ? (sd == 0 ? 14 : 6) - ilogbf(amax) : 0;
+        ex[sd] = ex[sd] > 64 ? 64 : ex[sd];
+        const float up = ldexpf(1.0f, ex[sd]);
+#pragma unroll
+        for (int z = 0; z < NH; ++z)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            h8 o;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const uint32_t x = word(raw[z][e], i);
+              o[2 * i] = (_Float16)(widen(x & 0xffffu) * up);
+              o[2 * i + 1] = (_Float16)(widen(x >> 16) * up);
+            }
+            if (sd == 0) {
+              put_key(buf, z, e, o);
+            } else {
+              put_value(buf, z, 2 * e, h2{o[0], o[1]}, h2{o[2], o[3]});
+              put_value(buf, z, 2 * e + 1, h2{o[4], o[5]}, h2{o[6], o[7]});
+            }
+          }
+      }
+      ks = ldexpf(1.0f, -ex[0]);
+      lv = (float)-ex[1];
+      iv = ldexpf(1.0f, ex[1]);
+    } else {                                                     // no tokens: zeros, and no weight
+      const h8 zero = {0, 0, 0, 0, 0, 0, 0, 0};
+      const h2 none = {0, 0};
+#pragma unroll
+      for (int z = 0; z < NH; ++z) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) put_key(buf, z, e, zero);
+#pragma unroll
+        for (int x = 0; x < 4; ++x) put_value(buf, z, x, none, none);
+      }
+      ks = 0.f;
+      lv = -INFINITY;
+      iv = 0.f;
+    }
+    if (lane == 0) *reinterpret_cast<f4*>(sinfo + (buf * 4 + w) * 4) = f4{ks, lv, iv, 0.f};
+  };
+
+  if (units > 0) {
+    load(0);
+    stage(0, 0);
+    if (units > 1) load(1);
   }
-  const int64_t o = (int64_t)(row0 + i) * V.hq + hq;
-  if (threadIdx.x < D) a.y[o * D + threadIdx.x] = float_to_elem<BF16>(l > 0.f ? out / l : 0.f);
-  if (threadIdx.x == 0 && a.lse != nullptr) a.lse[o] = l > 0.f ? (all + log2f(l)) * 0.693147180559945309f : -INFINITY;
+  __syncthreads();
+  for (int u = 0; u < units; ++u) {
+    const int buf = u & 1, t0 = u * kUnit;
+    if (t0 < most_seen) {
+      f16v s[2];
+#pragma unroll
+      for (int T = 0; T < 2; ++T) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[T][i] = 0.f;
+#pragma unroll
+        for (int x = 0; x < NS; ++x)
+          s[T] = __builtin_amdgcn_mfma_f32_32x32x16_f16(sk[(buf * (D / 8) + 2 * x + hh) * 64 + 32 * T + l32], q[x], s[T], 0, 0, 0);
+      }
+      float ks[4], lv[4], iv[4];
+#pragma unroll
+      for (int tt = 0; tt < 4; ++tt) {
+        const f4 f = *reinterpret_cast<const f4*>(sinfo + (buf * 4 + tt) * 4);
+        ks[tt] = f[0] * qs;
+        lv[tt] = f[1];
+        iv[tt] = f[2];
+      }
+      const int lim = sees < n ? sees : n;
+      const bool masked = t0 + kUnit > (least_seen < n ? least_seen : n);
+      float d[4][8];
+      const auto scores = [&](float ref) {
+#pragma unroll
+        for (int tt = 0; tt < 4; ++tt) {
+          const float o = lv[tt] - ref;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) d[tt][i] = fmaf(s[tt >> 1][8 * (tt & 1) + i], ks[tt], o);
+        }
+        if (masked) {
+#pragma unroll
+          for (int tt = 0; tt < 4; ++tt)
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+              if (t0 + 16 * tt + 8 * (i >> 2) + 4 * hh + (i & 3) >= lim) d[tt][i] = -INFINITY;
+        }
+        float mx = d[0][0];
+#pragma unroll
+        for (int tt = 0; tt < 4; ++tt)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) mx = fmaxf(mx, d[tt][i]);
+        return mx;
+      };
+      if (__any(scores(M) > 15.f)) {
+        const float next = fmaxf(M, halves_max(scores(0.f)) - 12.f), f = exp2_raw(M - next);
+        M = next;
+        l *= f;
+#pragma unroll
+        for (int c = 0; c < NC; ++c) y[c] *= f;
+        (void)scores(next);
+      }
+      h8 p[4];
+#pragma unroll
+      for (int tt = 0; tt < 4; ++tt) {
+        float e[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) e[i] = exp2_raw(d[tt][i]);
+        l = fmaf(((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7])), iv[tt], l);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) p[tt][i] = (_Float16)e[i];
+      }
+#pragma unroll
+      for (int tt = 0; tt < 4; ++tt)
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+          y[c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(sv[((buf * 4 + tt) * 2 + hh) * D + 32 * c + l32], p[tt], y[c], 0, 0, 0);
+    }
+    if (u + 1 < units) {
+      stage(u + 1, buf ^ 1);
+      if (u + 2 < units) load(u + 2);
+    }
+    __syncthreads();
+  }
+
+  l = halves_sum(l);
+  if (!live) return;
+  const int64_t at = (int64_t)(row0 + qi) * V.hq + hq;
+  const float inv = l > 0.f ? 1.0f / l : 0.f;
+#pragma unroll
+  for (int c = 0; c < NC; ++c)
+#pragma unroll
+    for (int i = 0; i < 16; i += 4) {
+      uint16_t o[4];
+#pragma unroll
+      for (int x = 0; x < 4; ++x) o[x] = V.elem == HCA_BF16 ? float_to_elem<true>(y[c][i + x] * inv) : float_to_elem<false>(y[c][i + x] * inv);
+      *reinterpret_cast<uint2*>(a.y + at * D + 32 * c + 8 * (i >> 2) + 4 * hh) = uint2{o[0] | (uint32_t)o[1] << 16, o[2] | (uint32_t)o[3] << 16};
+    }
+  if (hh == 0 && a.lse != nullptr) a.lse[at] = l > 0.f ? (M + log2f(l)) * 0.693147180559945309f : -INFINITY;
+}
+
+template <int D>
+static int32_t launch_tiles(const PagedView& V, const AttendArgs& a, hipStream_t st) {
+  constexpr int lds = 2 * 64 * D * 2 * 2 + 2 * 16 * 4;
+  const int64_t tiles = (int64_t)a.total * V.gqa / 128 + (a.total < V.n_seqs ? a.total : V.n_seqs);
+  const auto kernel = V.code == HCA_E4M3 ? paged_tile_kernel<D, true> : paged_tile_kernel<D, false>;
+  if (lds > 65536) {
+    static std::atomic<uint64_t> done[2];
+    const int32_t rc = lds_opt_in((const void*)kernel, lds, &done[V.code == HCA_E4M3]);
+    if (rc != HCA_OK) return rc;
+  }
+  kernel<<<(unsigned)(tiles * V.hkv), 256, lds, st>>>(V, a);
+  HCA_HIP(hipGetLastError());
+  return HCA_OK;
 }
 
 // Items per KV head that fill the chip once: two workgroups on each of its 256 compute units.
@@ -703,17 +908,6 @@ static int32_t launch_rows(const PagedView& V, const AttendArgs& a, int64_t max_
   }
 }
 
-template <int D, bool BF16>
-static int32_t launch_attend_rows(const PagedView& V, const AttendArgs& a, hipStream_t st) {
-  const dim3 grid((unsigned)a.total, (unsigned)V.hq);
-  if (V.code == HCA_E4M3)
-    paged_attend_kernel<D, BF16, true><<<grid, 256, 0, st>>>(V, a);
-  else
-    paged_attend_kernel<D, BF16, false><<<grid, 256, 0, st>>>(V, a);
-  HCA_HIP(hipGetLastError());
-  return HCA_OK;
-}
-
 }  // namespace hca
 
 using namespace hca;
@@ -748,8 +942,7 @@ int32_t hca_paged_attend(const hca_paged_shape* shape, const void* q, int64_t q_
   hipStream_t st = (hipStream_t)stream;
   if ((int64_t)(max_q < total_q ? max_q : total_q) * V.gqa <= 64)
     return V.D == 128 ? launch_rows<128>(V, a, max_len, workspace, st) : launch_rows<64>(V, a, max_len, workspace, st);
-  if (V.D == 128) return V.elem == HCA_BF16 ? launch_attend_rows<128, true>(V, a, st) : launch_attend_rows<128, false>(V, a, st);
-  return V.elem == HCA_BF16 ? launch_attend_rows<64, true>(V, a, st) : launch_attend_rows<64, false>(V, a, st);
+  return V.D == 128 ? launch_tiles<128>(V, a, st) : launch_tiles<64>(V, a, st);
 }
 
 }  // extern "C"
