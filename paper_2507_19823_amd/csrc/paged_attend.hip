@@ -18,6 +18,7 @@ struct AttendArgs {
 
 
 typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+typedef _Float16 h4 __attribute__((ext_vector_type(4)));
 typedef _Float16 h8 __attribute__((ext_vector_type(8)));
 typedef float f4 __attribute__((ext_vector_type(4)));
 
@@ -70,15 +71,17 @@ __device__ __forceinline__ float rows_sum(float x) {
 // the output's own step) with M 12 below the running maximum: the halves then reach 2^-26 below it as normal numbers, 2^-36 in
 // all, and M moves only when a score passes it by 15.  Their sum is taken in 32 bits before that, over w / vs.
 //
-// The tokens of a batch are divided evenly over the chip, from the lengths on the device: items of L units of 64
-// tokens, L such that there are about as many items as fit at once.
+// The tokens of a batch are divided evenly over the chip, from the lengths on the device: the sequences' units of 64 tokens
+// are numbered through, workgroup i takes units [i C, (i + 1) C), which may be the end of one sequence, some whole ones and
+// the beginning of another.  At most two of its pieces are not whole sequences: they go to its two places in the
+// workspace, and a second launch joins them.  (Items of one sequence each, of at most L units, left a short item behind
+// most sequences and a second round of workgroups: 32 sequences of 2.5 to 8 Ki took 83 us where this takes 61.)
 constexpr int kUnit = 64;
 
 struct SplitPlan {
-  int32_t want;         // items per KV head, about: a sequence's last one may be short, so there are up to n_seqs more
-  int32_t least;        // units per item at least
+  int32_t want;         // workgroups per KV head; 0: a workgroup per sequence, nothing to join
+  int32_t least;        // units per workgroup at least
 };
-constexpr int kWholeSeq = 1 << 25;                     // as `least`: more units than a sequence can have
 
 // tokens of sequence b, within the table
 __device__ __forceinline__ int seq_len(const PagedView& V, const AttendArgs& a, int b) {
@@ -92,15 +95,26 @@ __device__ __forceinline__ int seq_units(const PagedView& V, const AttendArgs& a
   const int u = ((seq_len(V, a, b) >> V.lp << V.lp) + kUnit - 1) / kUnit;
   return u > 1 ? u : 1;
 }
-__device__ __forceinline__ int split_len(const PagedView& V, const AttendArgs& a, const SplitPlan& sp) {
-  const int lane = threadIdx.x & 63;
-  if (sp.least >= kWholeSeq) return kWholeSeq;
-  uint64_t units = 0;
-  for (int b = lane; b < V.n_seqs; b += 64) units += (uint64_t)seq_units(V, a, b);
-  units = wave_scan_incl(units);
-  const int64_t all = (int64_t)((uint64_t)wave_last((uint32_t)(units >> 32)) << 32 | wave_last((uint32_t)units));
-  const int64_t L = (all + sp.want - 1) / sp.want;
-  return (int)(L > sp.least ? L : sp.least);
+// units per workgroup (all units together are fewer than 2^31: see paged_view)
+__device__ __forceinline__ int split_len(const SplitPlan& sp, uint32_t all) {
+  const int C = (int)((all + (uint32_t)sp.want - 1) / (uint32_t)sp.want);
+  return C > sp.least ? C : sp.least;
+}
+__device__ __forceinline__ uint32_t all_units(const PagedView& V, const AttendArgs& a) {
+  uint32_t units = 0;
+  for (int b = threadIdx.x & 63; b < V.n_seqs; b += 64) units += (uint32_t)seq_units(V, a, b);
+  return wave_sum(units);
+}
+
+// Four channels of output row `at` from the weighted values, the reference and the sum of the weights.
+template <int D>
+__device__ __forceinline__ void write_row(const PagedView& V, const AttendArgs& a, int64_t at, int ch, f4 o, float M, float sum) {
+  const float inv = sum > 0.f ? 1.0f / sum : 0.f;
+  uint16_t u[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) u[i] = V.elem == HCA_BF16 ? float_to_elem<true>(o[i] * inv) : float_to_elem<false>(o[i] * inv);
+  *reinterpret_cast<uint2*>(a.y + at * D + ch) = uint2{u[0] | (uint32_t)u[1] << 16, u[2] | (uint32_t)u[3] << 16};
+  if (ch == 0 && a.lse != nullptr) a.lse[at] = sum > 0.f ? (M + log2f(sum)) * 0.693147180559945309f : -INFINITY;
 }
 
 struct Partial {          // of one item, KV head and row: reference, sum; the weighted values follow in another array
@@ -108,403 +122,394 @@ struct Partial {          // of one item, KV head and row: reference, sum; the w
 };
 
 template <int D, int NT, bool E4M3>
-__global__ __launch_bounds__(256, NT == 1 ? 2 : 1) void paged_rows_kernel(PagedView V, AttendArgs a, SplitPlan sp, Partial* __restrict__ ml,
-                                                         float* __restrict__ part) {
+__global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void paged_rows_kernel(PagedView V, AttendArgs a, SplitPlan sp,
+                                                                          Partial* __restrict__ ml, float* __restrict__ part) {
   constexpr int NH = D / 64, NC = D / 16, COLS = 16 * NT;
+  constexpr int TT = NT == 1 ? 4 : 2, STEP = 16 * TT;  // tiles and tokens that a wave works on at a time
   extern __shared__ float lds[];                       // [4][COLS][D + 4], then M and l of each wave [4][COLS]
   const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int h = blockIdx.y;
-  const int L = split_len(V, a, sp);
-  int it;
-  const int b = paged_find(V.n_seqs, blockIdx.x, &it, [&](int s) { return (seq_units(V, a, s) + L - 1) / L; });
-  if (b >= V.n_seqs) return;
-  int row0;
-  const int m_all = paged_rows(a.cu, b, a.total, &row0);
-  const int m = m_all < a.max_q ? m_all : a.max_q;
-  const int n = seq_len(V, a, b), G = V.gqa;
-  const int whole = n >> V.lp << V.lp;
-  const int units = seq_units(V, a, b);
-  const int u0 = it * L, u1 = u0 + L < units ? u0 + L : units;
-  const bool last = u1 == units;
-  const int R = m * G;                                 // rows in use
+  const int h = blockIdx.y, G = V.gqa;
+  const int64_t side = V.side();
 
-  // this lane's query columns
-  h8 q[NT][NH][2];
-  float qs[NT];                                        // what a column's halves stand for, times sm_scale log2(e)
-  int sees[NT], least_seen = n;
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-    const int r = 16 * nt + l16;
-    const bool live = r < R;
-    const int qi = live ? r / G : 0, hq = h * G + (live ? r % G : 0);
-    const uint16_t* qp = a.q + (int64_t)(row0 + qi) * a.q_stride + (int64_t)hq * D;
-    const int upto = n - m_all + qi + 1;
-    sees[nt] = !(live && a.causal) ? n : upto > 0 ? upto : 0;
-    if (sees[nt] < least_seen) least_seen = sees[nt];
-    uint4 raw[NH][2];
-#pragma unroll
-    for (int x = 0; x < NH; ++x)
-#pragma unroll
-      for (int e = 0; e < 2; ++e)
-        raw[x][e] = live ? *reinterpret_cast<const uint4*>(qp + 64 * x + 16 * g + 8 * e) : uint4{0, 0, 0, 0};
-    qs[nt] = a.sm;
-    if (V.elem == HCA_BF16) {
-      float amax = 0.f;
-#pragma unroll
-      for (int x = 0; x < NH; ++x)
-#pragma unroll
-        for (int e = 0; e < 2; ++e)
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            amax = fmaxf(amax, fmaxf(fabsf(elem_to_float<true>(word(raw[x][e], i) & 0xffffu)), fabsf(elem_to_float<true>(word(raw[x][e], i) >> 16))));
-      amax = rows_max(amax);
-      int ex = amax > 0.f ? 14 - ilogbf(amax) : 0;
-      ex = ex > 100 ? 100 : ex;                        // largest magnitude in [2^14, 2^15)
-      const float up = ldexpf(1.0f, ex);
-      qs[nt] = ldexpf(a.sm, -ex);
-#pragma unroll
-      for (int x = 0; x < NH; ++x)
-#pragma unroll
-        for (int e = 0; e < 2; ++e)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            q[nt][x][e][2 * i] = (_Float16)(elem_to_float<true>(word(raw[x][e], i) & 0xffffu) * up);
-            q[nt][x][e][2 * i + 1] = (_Float16)(elem_to_float<true>(word(raw[x][e], i) >> 16) * up);
-          }
-    } else {
-#pragma unroll
-      for (int x = 0; x < NH; ++x)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) q[nt][x][e] = __builtin_bit_cast(h8, raw[x][e]);
-    }
-  }
-  least_seen = (int)wave_min((uint32_t)least_seen);
-
-  float M[NT], l[NT];
-  f4 y[NT][NC];
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-    M[nt] = -1e30f;
-    l[nt] = 0.f;
-#pragma unroll
-    for (int c = 0; c < NC; ++c) y[nt][c] = f4{0.f, 0.f, 0.f, 0.f};
+  // the workgroup's piece: from unit u of sequence b on, `left` units
+  int b, u, left;
+  if (sp.want == 0) {
+    b = paged_find(V.n_seqs, blockIdx.x, &u, [&](int s) { return seq_units(V, a, s) > 0 ? 1 : 0; });
+    if (b >= V.n_seqs) return;
+    left = seq_units(V, a, b);
+  } else {
+    const uint32_t all = all_units(V, a);
+    const int C = split_len(sp, all);
+    const int64_t U0 = (int64_t)blockIdx.x * C;
+    if (U0 >= all) return;
+    left = all - U0 < C ? (int)(all - U0) : C;
+    b = paged_find(V.n_seqs, (int)U0, &u, [&](int s) { return seq_units(V, a, s); });
   }
 
-  // TT tiles of 16 tokens from t0 on: scores -> weights (halves, ready for the second product)
-  const auto weigh = [&](auto tiles, f4(&s)[NT][decltype(tiles)::value], const float* ks, const float* lv, const float* iv, int t0,
-                         int end, h2(&p)[NT][decltype(tiles)::value][2]) {
-    constexpr int TT = decltype(tiles)::value;
-    const bool masked = t0 + 16 * TT > (least_seen < end ? least_seen : end);
+  for (bool first = true;; first = false) {
+    const int units = seq_units(V, a, b);
+    const int ue = units - u < left ? units : u + left;
+    int row0;
+    const int m_all = paged_rows(a.cu, b, a.total, &row0);
+    const int m = m_all < a.max_q ? m_all : a.max_q;
+    const int n = seq_len(V, a, b), whole = n >> V.lp << V.lp;
+    const int R = m * G;                               // rows in use
+
+    // whole pages: steps of STEP tokens, wave w takes every fourth
+    const int t_begin = u * kUnit, t_end = ue * kUnit < whole ? ue * kUnit : whole;
+    const int steps = t_end > t_begin ? (t_end - t_begin + STEP - 1) / STEP : 0;
+    const int nk = steps > w ? (steps - w + 3) / 4 : 0;
+    constexpr int LS = TT == 4 ? 6 : 5;
+    const int lpe = V.lp < LS ? V.lp : LS;              // pages smaller than a step: STEP >> lpe of them
+    const int per = STEP >> lpe, group = 64 / per;      // pages per step, steps whose pages the lanes hold
+    const int32_t* table = a.tables + (int64_t)b * V.max_pages;
+    // lane j holds page j % per of the wave's step k0 + j / per: its number (-1: no tokens) and scales.  The next group's
+    // numbers are asked for when a group begins, its scales one step later.
+    const auto ask_id = [&](int k0) {
+      const int k = k0 + lane / per, t = t_begin + (w + 4 * k) * STEP + (lane % per << lpe);
+      return k < nk && t < t_end ? table[t >> V.lp] : -1;
+    };
+    const auto ask_scale = [&](int id) {
+      return id >= 0 && id < V.n_pages ? *reinterpret_cast<const float2*>(a.scale + ((int64_t)id * V.hkv + h) * 2) : float2{0.f, 1.f};
+    };
+    int id = ask_id(0), next_id = -1;
+
+    // this lane's query columns
+    h8 q[NT][NH][2];
+    float qs[NT];                                      // what a column's halves stand for, times sm_scale log2(e)
+    int sees[NT], least_seen = n;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-      float d[TT][4];
-      const int lim = sees[nt] < end ? sees[nt] : end;
-      const auto scores = [&](float ref) {
-#pragma unroll
-        for (int tt = 0; tt < TT; ++tt) {
-          const float c = ks[tt] * qs[nt], o = lv[tt] - ref;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) d[tt][i] = fmaf(s[nt][tt][i], c, o);
-        }
-        if (masked) {
-#pragma unroll
-          for (int tt = 0; tt < TT; ++tt)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-              if (t0 + 16 * tt + 4 * g + i >= lim) d[tt][i] = -INFINITY;
-        }
-        float mx = d[0][0];
-#pragma unroll
-        for (int tt = 0; tt < TT; ++tt)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) mx = fmaxf(mx, d[tt][i]);
-        return mx;
-      };
-      if (__any(scores(M[nt]) > 15.f)) {
-        const float top = rows_max(scores(0.f)) - 12.f;
-        const float next = fmaxf(M[nt], top), f = exp2_raw(M[nt] - next);
-        M[nt] = next;
-        l[nt] *= f;
-#pragma unroll
-        for (int c = 0; c < NC; ++c) y[nt][c] *= f;
-        (void)scores(next);
-      }
-#pragma unroll
-      for (int tt = 0; tt < TT; ++tt) {
-        float e[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) e[i] = exp2_raw(d[tt][i]);
-        l[nt] = fmaf((e[0] + e[1]) + (e[2] + e[3]), iv[tt], l[nt]);
-        p[nt][tt][0] = h2{(_Float16)e[0], (_Float16)e[1]};
-        p[nt][tt][1] = h2{(_Float16)e[2], (_Float16)e[3]};
-      }
-    }
-  };
-
-  // ---- whole pages: units u0 + w, u0 + w + 4, ...
-  const int lpe = V.lp < 6 ? V.lp : 6;                  // pages smaller than a unit: 64 >> lpe of them per unit
-  const int per = 64 >> lpe, group = 64 / per;          // pages per unit, units whose pages the lanes hold
-  const int nk = u1 - u0 > w ? (u1 - u0 - w + 3) / 4 : 0;
-  const int32_t* table = a.tables + (int64_t)b * V.max_pages;
-  const int64_t side = V.side();
-  // lane j holds page j % per of the wave's unit k0 + j / per: number (-1: no tokens), scales
-  struct Info { int id; float ks, vs; };
-  const auto fetch = [&](int k0) {
-    const int k = k0 + lane / per, t = (u0 + w + 4 * k) * kUnit + (lane % per << lpe);
-    Info f{-1, 0.f, 1.f};
-    if (k < nk && t < whole) {
-      const int id = table[t >> V.lp];
-      if (id >= 0 && id < V.n_pages) {
-        const float2 sc = *reinterpret_cast<const float2*>(a.scale + ((int64_t)id * V.hkv + h) * 2);
-        f = Info{id, sc.x, sc.y};
-      }
-    }
-    return f;
-  };
-  Info cur = fetch(0);
-  float cur_lv = log2_raw(cur.vs), cur_iv = 1.0f / cur.vs;
-  uint4 kw[4][NH], vw[4][NH];
-  const auto address = [&](int k, int tt) {             // first key byte of tile tt of unit k; null: no tokens
-    const int id = __builtin_amdgcn_readlane(cur.id, (k % group) * per + (16 * tt >> lpe));
-    const int t = (u0 + w + 4 * k) * kUnit + 16 * tt;
-    return id < 0 ? (const uint8_t*)nullptr : a.kv + ((int64_t)id * V.hkv + h) * 2 * side + (t & (V.P - 1)) * D;
-  };
-  const auto load = [&](int k, uint4(&x)[4][NH], int64_t off) {
-#pragma unroll
-    for (int tt = 0; tt < 4; ++tt) {
-      const uint8_t* p = address(k, tt);
-#pragma unroll
-      for (int z = 0; z < NH; ++z)
-        x[tt][z] = p != nullptr ? load_stream16(reinterpret_cast<const uint4*>(p + off) + z * 64 + lane) : uint4{0, 0, 0, 0};
-    }
-  };
-  if (nk > 0) {
-    load(0, kw, 0);
-    load(0, vw, side);
-  }
-  for (int k = 0; k < nk; ++k) {
-    float ks[4], lv[4], iv[4];
-#pragma unroll
-    for (int tt = 0; tt < 4; ++tt) {
-      const int j = (k % group) * per + (16 * tt >> lpe);
-      const bool none = __builtin_amdgcn_readlane(cur.id, j) < 0;
-      ks[tt] = lane_value(cur.ks, j);
-      lv[tt] = none ? -INFINITY : lane_value(cur_lv, j);
-      iv[tt] = none ? 0.f : lane_value(cur_iv, j);
-    }
-    f4 s[NT][4];
-#pragma unroll
-    for (int tt = 0; tt < 4; ++tt) {
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) s[nt][tt] = f4{0.f, 0.f, 0.f, 0.f};
+      const int r = 16 * nt + l16;
+      const bool live = r < R;
+      const int qi = live ? r / G : 0, hq = h * G + (live ? r % G : 0);
+      const uint16_t* qp = a.q + (int64_t)(row0 + qi) * a.q_stride + (int64_t)hq * D;
+      const int upto = n - m_all + qi + 1;
+      sees[nt] = !(live && a.causal) ? n : upto > 0 ? upto : 0;
+      if (sees[nt] < least_seen) least_seen = sees[nt];
+      uint4 raw[NH][2];
 #pragma unroll
       for (int x = 0; x < NH; ++x)
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const h8 kk = codes_to_halves<E4M3>(word(kw[tt][x], 2 * e), word(kw[tt][x], 2 * e + 1));
+        for (int e = 0; e < 2; ++e)
+          raw[x][e] = live ? *reinterpret_cast<const uint4*>(qp + 64 * x + 16 * g + 8 * e) : uint4{0, 0, 0, 0};
+      qs[nt] = a.sm;
+      if (V.elem == HCA_BF16) {
+        float amax = 0.f;
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt) s[nt][tt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kk, q[nt][x][e], s[nt][tt], 0, 0, 0);
-        }
-    }
-    const bool more = k + 1 < nk;
-    if (more) {
-      if ((k + 1) % group == 0) {
-        cur = fetch(k + 1);
-        cur_lv = log2_raw(cur.vs);
-        cur_iv = 1.0f / cur.vs;
+        for (int x = 0; x < NH; ++x)
+#pragma unroll
+          for (int e = 0; e < 2; ++e)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              amax = fmaxf(amax, fmaxf(fabsf(elem_to_float<true>(word(raw[x][e], i) & 0xffffu)), fabsf(elem_to_float<true>(word(raw[x][e], i) >> 16))));
+        amax = rows_max(amax);
+        int ex = amax > 0.f ? 14 - ilogbf(amax) : 0;
+        ex = ex > 100 ? 100 : ex;                      // largest magnitude in [2^14, 2^15)
+        const float up = ldexpf(1.0f, ex);
+        qs[nt] = ldexpf(a.sm, -ex);
+#pragma unroll
+        for (int x = 0; x < NH; ++x)
+#pragma unroll
+          for (int e = 0; e < 2; ++e)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              q[nt][x][e][2 * i] = (_Float16)(elem_to_float<true>(word(raw[x][e], i) & 0xffffu) * up);
+              q[nt][x][e][2 * i + 1] = (_Float16)(elem_to_float<true>(word(raw[x][e], i) >> 16) * up);
+            }
+      } else {
+#pragma unroll
+        for (int x = 0; x < NH; ++x)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) q[nt][x][e] = __builtin_bit_cast(h8, raw[x][e]);
       }
-      load(k + 1, kw, 0);
     }
-    h2 p[NT][4][2];
-    weigh(std::integral_constant<int, 4>{}, s, ks, lv, iv, (u0 + w + 4 * k) * kUnit, whole, p);
-#pragma unroll
-    for (int pr = 0; pr < 2; ++pr) {
-      h8 pb[NT];
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-        pb[nt] = h8{p[nt][2 * pr][0].x, p[nt][2 * pr][0].y, p[nt][2 * pr][1].x, p[nt][2 * pr][1].y,
-                    p[nt][2 * pr + 1][0].x, p[nt][2 * pr + 1][0].y, p[nt][2 * pr + 1][1].x, p[nt][2 * pr + 1][1].y};
-#pragma unroll
-      for (int c = 0; c < NC; ++c) {
-        const h8 vv = codes_to_halves<E4M3>(word(vw[2 * pr][c >> 2], c & 3), word(vw[2 * pr + 1][c >> 2], c & 3));
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) y[nt][c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vv, pb[nt], y[nt][c], 0, 0, 0);
-      }
-    }
-    if (more) load(k + 1, vw, side);
-  }
+    least_seen = (int)wave_min((uint32_t)least_seen);
 
-  // ---- open rows, two tiles per wave, in the last item: the same with halves made from the rows themselves
-  if (last) {
-    const int t0 = whole + 32 * w;
-    const auto widen = [&](uint32_t bits) { return V.elem == HCA_BF16 ? elem_to_float<true>(bits) : elem_to_float<false>(bits); };
-    if (t0 < n) {
-      const uint16_t* kp = a.open + ((int64_t)b * V.hkv + h) * 2 * side + (t0 & (V.P - 1)) * D;
-      const bool two = t0 + 16 < n;                     // (a page of 16 has no second tile)
-      h8 kk[2][NH][2], vv[2][NH][2];
-      float ks[2], lv[2], iv[2];
+    float M[NT], l[NT];
+    f4 y[NT][NC];
 #pragma unroll
-      for (int sd = 0; sd < 2; ++sd) {
-        uint4 raw[2][NH][2];
+    for (int nt = 0; nt < NT; ++nt) {
+      M[nt] = -1e30f;
+      l[nt] = 0.f;
 #pragma unroll
-        for (int tt = 0; tt < 2; ++tt)
+      for (int c = 0; c < NC; ++c) y[nt][c] = f4{0.f, 0.f, 0.f, 0.f};
+    }
+
+    // X tiles of 16 tokens from t0 on: scores -> weights (halves, ready for the second product)
+    const auto weigh = [&](auto tiles, f4(&s)[NT][decltype(tiles)::value], const float* ks, const float* lv, const float* iv, int t0,
+                           int end, h2(&p)[NT][decltype(tiles)::value][2]) {
+      constexpr int X = decltype(tiles)::value;
+      const bool masked = t0 + 16 * X > (least_seen < end ? least_seen : end);
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        float d[X][4];
+        const int lim = sees[nt] < end ? sees[nt] : end;
+        const auto scores = [&](float ref) {
+#pragma unroll
+          for (int tt = 0; tt < X; ++tt) {
+            const float c = ks[tt] * qs[nt], o = lv[tt] - ref;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) d[tt][i] = fmaf(s[nt][tt][i], c, o);
+          }
+          if (masked) {
+#pragma unroll
+            for (int tt = 0; tt < X; ++tt)
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+                if (t0 + 16 * tt + 4 * g + i >= lim) d[tt][i] = -INFINITY;
+          }
+          float mx = d[0][0];
+#pragma unroll
+          for (int tt = 0; tt < X; ++tt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) mx = fmaxf(mx, d[tt][i]);
+          return mx;
+        };
+        if (__any(scores(M[nt]) > 15.f)) {
+          const float top = rows_max(scores(0.f)) - 12.f;
+          const float next = fmaxf(M[nt], top), f = exp2_raw(M[nt] - next);
+          M[nt] = next;
+          l[nt] *= f;
+#pragma unroll
+          for (int c = 0; c < NC; ++c) y[nt][c] *= f;
+          (void)scores(next);
+        }
+#pragma unroll
+        for (int tt = 0; tt < X; ++tt) {
+          float e[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) e[i] = exp2_raw(d[tt][i]);
+          l[nt] = fmaf((e[0] + e[1]) + (e[2] + e[3]), iv[tt], l[nt]);
+          p[nt][tt][0] = h2{(_Float16)e[0], (_Float16)e[1]};
+          p[nt][tt][1] = h2{(_Float16)e[2], (_Float16)e[3]};
+        }
+      }
+    };
+
+    uint4 kw[TT][NH], vw[TT][NH];
+    // codes of step k; `off`: 0 keys, side values
+    const auto load = [&](int k, uint4(&x)[TT][NH], int64_t off) {
+#pragma unroll
+      for (int tt = 0; tt < TT; ++tt) {
+        const int pg = __builtin_amdgcn_readlane(id, (k % group) * per + (16 * tt >> lpe));
+        const int t = t_begin + (w + 4 * k) * STEP + 16 * tt;
+        const uint8_t* p = a.kv + ((int64_t)pg * V.hkv + h) * 2 * side + (t & (V.P - 1)) * D + off;
+        const bool there = pg >= 0 && pg < V.n_pages;
+#pragma unroll
+        for (int z = 0; z < NH; ++z)
+          x[tt][z] = there ? load_stream16(reinterpret_cast<const uint4*>(p) + z * 64 + lane) : uint4{0, 0, 0, 0};
+      }
+    };
+    float2 sc = float2{0.f, 1.f}, next_sc = float2{0.f, 1.f};
+    if (nk > 0) {
+      load(0, kw, 0);
+      load(0, vw, side);
+      sc = ask_scale(id);
+    }
+    float sc_lv = log2_raw(sc.y), sc_iv = 1.0f / sc.y;
+    for (int k = 0; k < nk; ++k) {
+      const int kg = k % group;
+      if (kg == 0) next_id = ask_id(k + group);
+      if (kg == 1) next_sc = ask_scale(next_id);
+      float ks[TT], lv[TT], iv[TT];
+#pragma unroll
+      for (int tt = 0; tt < TT; ++tt) {
+        const int j = kg * per + (16 * tt >> lpe), pg = __builtin_amdgcn_readlane(id, j);
+        const bool there = pg >= 0 && pg < V.n_pages;
+        ks[tt] = lane_value(sc.x, j);
+        lv[tt] = there ? lane_value(sc_lv, j) : -INFINITY;
+        iv[tt] = there ? lane_value(sc_iv, j) : 0.f;
+      }
+      f4 s[NT][TT];
+#pragma unroll
+      for (int tt = 0; tt < TT; ++tt) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) s[nt][tt] = f4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int x = 0; x < NH; ++x)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const h8 kk = codes_to_halves<E4M3>(word(kw[tt][x], 2 * e), word(kw[tt][x], 2 * e + 1));
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) s[nt][tt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kk, q[nt][x][e], s[nt][tt], 0, 0, 0);
+          }
+      }
+      const bool more = k + 1 < nk;
+      if (more) {
+        if (kg + 1 == group) {
+          id = next_id;
+          sc = next_sc;
+          sc_lv = log2_raw(sc.y);
+          sc_iv = 1.0f / sc.y;
+        }
+        load(k + 1, kw, 0);
+      }
+      h2 p[NT][TT][2];
+      weigh(std::integral_constant<int, TT>{}, s, ks, lv, iv, t_begin + (w + 4 * k) * STEP, t_end, p);
+#pragma unroll
+      for (int pr = 0; pr < TT / 2; ++pr) {
+        h8 pb[NT];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+          pb[nt] = h8{p[nt][2 * pr][0].x, p[nt][2 * pr][0].y, p[nt][2 * pr][1].x, p[nt][2 * pr][1].y,
+                      p[nt][2 * pr + 1][0].x, p[nt][2 * pr + 1][0].y, p[nt][2 * pr + 1][1].x, p[nt][2 * pr + 1][1].y};
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+          const h8 vv = codes_to_halves<E4M3>(word(vw[2 * pr][c >> 2], c & 3), word(vw[2 * pr + 1][c >> 2], c & 3));
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) y[nt][c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vv, pb[nt], y[nt][c], 0, 0, 0);
+        }
+      }
+      if (more) load(k + 1, vw, side);
+    }
+
+    // open rows, a tile at a time, where the piece ends the sequence: the same with halves made from the rows themselves
+    if (ue == units) {
+      const auto widen = [&](uint32_t bits) { return V.elem == HCA_BF16 ? elem_to_float<true>(bits) : elem_to_float<false>(bits); };
+      for (int t0 = whole + 16 * w; t0 < n; t0 += 64) {
+        const uint16_t* kp = a.open + ((int64_t)b * V.hkv + h) * 2 * side + (t0 & (V.P - 1)) * D;
+        float ks, lv, iv;
+        f4 s[NT][1];
+        h2 p[NT][1][2];
+#pragma unroll
+        for (int sd = 0; sd < 2; ++sd) {
+          uint4 raw[NH][2];
+          float amax = 0.f;
 #pragma unroll
           for (int x = 0; x < NH; ++x)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-              uint4 v = uint4{0, 0, 0, 0};
-              if (tt == 0 || two) v = *(reinterpret_cast<const uint4*>(kp + sd * side + tt * 16 * D + (x * 64 + lane) * 16) + e);
+              const uint4 v = *(reinterpret_cast<const uint4*>(kp + sd * side + (x * 64 + lane) * 16) + e);
               // rows behind the last token may hold anything: keys by lane, values by place in the tile
-              const int t = t0 + 16 * tt;
               uint32_t wd[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
               for (int i = 0; i < 4; ++i) {
-                const int a0 = sd == 0 ? t + l16 : t + 4 * g + 2 * (i & 1), a1 = sd == 0 ? t + l16 : a0 + 1;
+                const int a0 = sd == 0 ? t0 + l16 : t0 + 4 * g + 2 * (i & 1), a1 = sd == 0 ? t0 + l16 : a0 + 1;
                 wd[i] = (a0 < n ? wd[i] & 0xffffu : 0u) | (a1 < n ? wd[i] & 0xffff0000u : 0u);
+                amax = fmaxf(amax, fmaxf(fabsf(widen(wd[i] & 0xffffu)), fabsf(widen(wd[i] >> 16))));
               }
-              raw[tt][x][e] = uint4{wd[0], wd[1], wd[2], wd[3]};
+              raw[x][e] = uint4{wd[0], wd[1], wd[2], wd[3]};
             }
-        // a power of two brings them to the halves' range: bfloat16 keys to the top of it (below it nothing is lost that
-        // counts), values to that of codes, so that their weights are no smaller than a whole page's
-        int ex = 0;
-        if (sd == 1 || V.elem == HCA_BF16) {
-          float amax = 0.f;
-#pragma unroll
-          for (int tt = 0; tt < 2; ++tt)
-#pragma unroll
-            for (int x = 0; x < NH; ++x)
-#pragma unroll
-              for (int e = 0; e < 2; ++e)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                  const uint32_t u = word(raw[tt][x][e], i);
-                  amax = fmaxf(amax, fmaxf(fabsf(widen(u & 0xffffu)), fabsf(widen(u >> 16))));
-                }
+          // a power of two brings them to the halves' range: bfloat16 keys to the top of it (below it nothing is lost
+          // that counts), values to that of codes, so that their weights are no smaller than a whole page's
           amax = wave_max(amax);
-          ex = amax > 0.f ? (sd == 0 ? 14 : 6) - ilogbf(amax) : 0;
+          int ex = amax > 0.f && (sd == 1 || V.elem == HCA_BF16) ? (sd == 0 ? 14 : 6) - ilogbf(amax) : 0;
           ex = ex > 64 ? 64 : ex;
-        }
-        const float up = ldexpf(1.0f, ex);
-#pragma unroll
-        for (int tt = 0; tt < 2; ++tt)
+          const float up = ldexpf(1.0f, ex);
+          h8 o[NH][2];
 #pragma unroll
           for (int x = 0; x < NH; ++x)
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              h8 o = __builtin_bit_cast(h8, raw[tt][x][e]);
-              if (sd == 1 || V.elem == HCA_BF16) {
+            for (int e = 0; e < 2; ++e)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                  const uint32_t u = word(raw[tt][x][e], i);
-                  o[2 * i] = (_Float16)(widen(u & 0xffffu) * up);
-                  o[2 * i + 1] = (_Float16)(widen(u >> 16) * up);
-                }
+              for (int i = 0; i < 4; ++i) {
+                o[x][e][2 * i] = (_Float16)(widen(word(raw[x][e], i) & 0xffffu) * up);
+                o[x][e][2 * i + 1] = (_Float16)(widen(word(raw[x][e], i) >> 16) * up);
               }
-              (sd == 0 ? kk : vv)[tt][x][e] = o;
+          if (sd == 0) {
+            ks = ldexpf(1.0f, -ex);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+              s[nt][0] = f4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+              for (int x = 0; x < NH; ++x)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) s[nt][0] = __builtin_amdgcn_mfma_f32_16x16x32_f16(o[x][e], q[nt][x][e], s[nt][0], 0, 0, 0);
             }
-        if (sd == 0) ks[0] = ks[1] = ldexpf(1.0f, -ex);
-        else {
-          lv[0] = lv[1] = (float)-ex;
-          iv[0] = iv[1] = up;
-        }
-      }
-      f4 s[NT][2];
+          } else {
+            lv = (float)-ex;
+            iv = up;
+            weigh(std::integral_constant<int, 1>{}, s, &ks, &lv, &iv, t0, n, p);
 #pragma unroll
-      for (int tt = 0; tt < 2; ++tt)
+            for (int nt = 0; nt < NT; ++nt) {
+              const h4 pb = h4{p[nt][0][0].x, p[nt][0][0].y, p[nt][0][1].x, p[nt][0][1].y};
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          s[nt][tt] = f4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-          for (int x = 0; x < NH; ++x)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) s[nt][tt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kk[tt][x][e], q[nt][x][e], s[nt][tt], 0, 0, 0);
-        }
-      h2 p[NT][2][2];
-      weigh(std::integral_constant<int, 2>{}, s, ks, lv, iv, t0, n, p);
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        const h8 pb = h8{p[nt][0][0].x, p[nt][0][0].y, p[nt][0][1].x, p[nt][0][1].y,
-                         p[nt][1][0].x, p[nt][1][0].y, p[nt][1][1].x, p[nt][1][1].y};
-#pragma unroll
-        for (int c = 0; c < NC; ++c) {
-          // channels 16 c + l16: numbers 4 (c % 4) .. + 3 of the lane's sixteen
-          const h8 v0 = vv[0][c >> 2][(c & 3) >> 1], v1 = vv[1][c >> 2][(c & 3) >> 1];
-          const int o = 4 * (c & 1);
-          y[nt][c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(
-              h8{v0[o], v0[o + 1], v0[o + 2], v0[o + 3], v1[o], v1[o + 1], v1[o + 2], v1[o + 3]}, pb, y[nt][c], 0, 0, 0);
+              for (int c = 0; c < NC; ++c) {           // channels 16 c + l16: numbers 4 (c % 4) .. + 3 of the lane's sixteen
+                const h8 v = o[c >> 2][(c & 3) >> 1];
+                const int z = 4 * (c & 1);
+                y[nt][c] = __builtin_amdgcn_mfma_f32_16x16x16f16(h4{v[z], v[z + 1], v[z + 2], v[z + 3]}, pb, y[nt][c], 0, 0, 0);
+              }
+            }
+          }
         }
       }
     }
-  }
 
-  // ---- the four waves' results are joined
-  constexpr int RS = D + 4;
-  float* sM = lds + 4 * COLS * RS;
-  float* sl = sM + 4 * COLS;
+    // the four waves' results are joined
+    constexpr int RS = D + 4;
+    float* sM = lds + 4 * COLS * RS;
+    float* sl = sM + 4 * COLS;
 #pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-    const float sum = rows_sum(l[nt]);
-    if (g == 0) {
-      sM[w * COLS + 16 * nt + l16] = M[nt];
-      sl[w * COLS + 16 * nt + l16] = sum;
+    for (int nt = 0; nt < NT; ++nt) {
+      const float sum = rows_sum(l[nt]);
+      if (g == 0) {
+        sM[w * COLS + 16 * nt + l16] = M[nt];
+        sl[w * COLS + 16 * nt + l16] = sum;
+      }
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+        *reinterpret_cast<f4*>(lds + (w * COLS + 16 * nt + l16) * RS + 16 * c + 4 * g) = y[nt][c];
     }
+    __syncthreads();
+    const bool only = u == 0 && ue == units;
+    constexpr int TPR = D / 4;                          // threads per row, four channels each
+    for (int r = threadIdx.x / TPR; r < R; r += 256 / TPR) {
+      const int ch = threadIdx.x % TPR * 4;
+      const float top = fmaxf(fmaxf(sM[r], sM[COLS + r]), fmaxf(sM[2 * COLS + r], sM[3 * COLS + r]));
+      float sum = 0.f;
+      f4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int c = 0; c < NC; ++c)
-      *reinterpret_cast<f4*>(lds + (w * COLS + 16 * nt + l16) * RS + 16 * c + 4 * g) = y[nt][c];
-  }
-  __syncthreads();
-  const bool only = units <= L;
-  constexpr int TPR = D / 4;                            // threads per row, four channels each
-  for (int r = threadIdx.x / TPR; r < R; r += 256 / TPR) {
-    const int ch = threadIdx.x % TPR * 4;
-    const float all = fmaxf(fmaxf(sM[r], sM[COLS + r]), fmaxf(sM[2 * COLS + r], sM[3 * COLS + r]));
-    float sum = 0.f;
-    f4 o = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int x = 0; x < 4; ++x) {
-      const float f = exp2_raw(sM[x * COLS + r] - all);
-      sum = fmaf(sl[x * COLS + r], f, sum);
-      o += *reinterpret_cast<const f4*>(lds + (x * COLS + r) * RS + ch) * f;
+      for (int x = 0; x < 4; ++x) {
+        const float f = exp2_raw(sM[x * COLS + r] - top);
+        sum = fmaf(sl[x * COLS + r], f, sum);
+        o += *reinterpret_cast<const f4*>(lds + (x * COLS + r) * RS + ch) * f;
+      }
+      if (only) {
+        write_row<D>(V, a, (int64_t)(row0 + r / G) * V.hq + h * G + r % G, ch, o, top, sum);
+      } else {
+        const int64_t at = ((2 * (int64_t)blockIdx.x + (first ? 0 : 1)) * V.hkv + h) * COLS + r;
+        *reinterpret_cast<f4*>(part + at * D + ch) = o;
+        if (ch == 0) ml[at] = Partial{top, sum};
+      }
     }
-    if (only) {
-      const int64_t at = (int64_t)(row0 + r / G) * V.hq + h * G + r % G;
-      const float inv = sum > 0.f ? 1.0f / sum : 0.f;
-      uint16_t u[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) u[i] = V.elem == HCA_BF16 ? float_to_elem<true>(o[i] * inv) : float_to_elem<false>(o[i] * inv);
-      *reinterpret_cast<uint2*>(a.y + at * D + ch) = uint2{u[0] | (uint32_t)u[1] << 16, u[2] | (uint32_t)u[3] << 16};
-      if (ch == 0 && a.lse != nullptr) a.lse[at] = sum > 0.f ? (all + log2f(sum)) * 0.693147180559945309f : -INFINITY;
-    } else {
-      const int64_t at = ((int64_t)blockIdx.x * V.hkv + h) * COLS + r;
-      *reinterpret_cast<f4*>(part + at * D + ch) = o;
-      if (ch == 0) ml[at] = Partial{all, sum};
-    }
+    left -= ue - u;
+    if (left <= 0) return;
+    do ++b; while (b < V.n_seqs && seq_units(V, a, b) == 0);
+    if (b >= V.n_seqs) return;
+    u = 0;
+    __syncthreads();                                    // LDS is free again
   }
 }
 
-// Joins the items of sequences that have several.  One workgroup per query row and head, items in a fixed order.
+// Joins the pieces of sequences that have several.  One workgroup per query row and head, pieces in a fixed order.
 template <int D>
 __global__ __launch_bounds__(256) void paged_join_kernel(PagedView V, AttendArgs a, SplitPlan sp, int cols, const Partial* __restrict__ ml,
                                                          const float* __restrict__ part) {
-  constexpr int TPR = D / 4, NG = 256 / TPR;            // groups of threads, each with every NG-th item
+  constexpr int TPR = D / 4, NG = 256 / TPR;            // groups of threads, each with every NG-th piece
   __shared__ f4 s_o[NG][TPR];
   __shared__ float s_l[NG];
   const int hq = blockIdx.y, h = hq / V.gqa, lane = threadIdx.x & 63;
   int i;
   const int b = paged_find(V.n_seqs, blockIdx.x, &i, [&](int s) { int f; return paged_rows(a.cu, s, a.total, &f); });
   if (b >= V.n_seqs || i >= a.max_q) return;
-  const int L = split_len(V, a, sp);
-  const int count = (seq_units(V, a, b) + L - 1) / L;
+  uint32_t all = 0, before = 0;
+  for (int s = lane; s < V.n_seqs; s += 64) {
+    const uint32_t c = (uint32_t)seq_units(V, a, s);
+    all += c;
+    before += s < b ? c : 0;
+  }
+  const int C = split_len(sp, wave_sum(all));
+  const int S = (int)wave_sum(before), E = S + seq_units(V, a, b);       // the sequence's units
+  const int i0 = S / C, count = (E - 1) / C - i0 + 1;                    // its workgroups
   if (count <= 1) return;
-  uint32_t before = 0;
-  for (int s = lane; s < b; s += 64) before += (uint32_t)((seq_units(V, a, s) + L - 1) / L);
-  const int first = (int)wave_sum(before);
   int row0;
   (void)paged_rows(a.cu, b, a.total, &row0);
   const int r = i * V.gqa + hq % V.gqa;
   const int grp = threadIdx.x / TPR, ch = threadIdx.x % TPR * 4;
-  const auto at = [&](int k) { return ((int64_t)(first + k) * V.hkv + h) * cols + r; };
+  const int late = S > i0 * C ? 1 : 0;                                   // the first piece is not its workgroup's first
+  const auto at = [&](int k) { return ((2 * (int64_t)(i0 + k) + (k == 0 ? late : 0)) * V.hkv + h) * cols + r; };
   float M = -1e30f;
   for (int k = lane; k < count; k += 64) M = fmaxf(M, ml[at(k)].M);
   M = wave_max(M);
@@ -526,13 +531,7 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedView V, AttendArgs
     o += s_o[x][ch / 4];
     sum += s_l[x];
   }
-  const int64_t out = (int64_t)(row0 + i) * V.hq + hq;
-  const float inv = sum > 0.f ? 1.0f / sum : 0.f;
-  uint16_t u[4];
-#pragma unroll
-  for (int x = 0; x < 4; ++x) u[x] = V.elem == HCA_BF16 ? float_to_elem<true>(o[x] * inv) : float_to_elem<false>(o[x] * inv);
-  *reinterpret_cast<uint2*>(a.y + out * D + ch) = uint2{u[0] | (uint32_t)u[1] << 16, u[2] | (uint32_t)u[3] << 16};
-  if (ch == 0 && a.lse != nullptr) a.lse[out] = sum > 0.f ? (M + log2f(sum)) * 0.693147180559945309f : -INFINITY;
+  write_row<D>(V, a, (int64_t)(row0 + i) * V.hq + hq, ch, o, M, sum);
 }
 
 // ---- many query rows: the matrix cores are the bound -------------------------------------------------
@@ -866,11 +865,10 @@ static int32_t launch_tiles(const PagedView& V, const AttendArgs& a, hipStream_t
   return HCA_OK;
 }
 
-// Items per KV head that fill the chip once: two workgroups on each of its 256 compute units.
+// Workgroups per KV head that fill the chip once: two on each of its 256 compute units.
 static int rows_want(const PagedView& V) { return V.hkv >= 512 ? 1 : 512 / V.hkv; }
-constexpr int kOneItem = 1024;      // sequences up to this length are one item, and nothing has to be joined
+constexpr int kOneItem = 1024;      // sequences up to this length are one piece, and nothing has to be joined
 
-static int64_t rows_items(const PagedView& V, int64_t total_q) { return rows_want(V) + (total_q < V.n_seqs ? total_q : V.n_seqs); }
 static int rows_cols(const PagedView& V, int max_q) {
   const int64_t R = (int64_t)max_q * V.gqa;
   return R <= 16 ? 16 : R <= 32 ? 32 : 64;
@@ -880,11 +878,11 @@ template <int D, int NT>
 static int32_t launch_rows_nt(const PagedView& V, const AttendArgs& a, int64_t max_len, void* ws, hipStream_t st) {
   constexpr int lds = 4 * 16 * NT * (D + 4 + 2) * 4;
   const bool one = max_len <= kOneItem;
-  const int64_t items = one ? V.n_seqs : rows_items(V, a.total);
-  const SplitPlan sp{rows_want(V), one ? kWholeSeq : 4};
+  const SplitPlan sp{one ? 0 : rows_want(V), 4};
+  const int64_t rows = 2 * (int64_t)rows_want(V) * V.hkv * 16 * NT;
   Partial* ml = (Partial*)ws;
-  float* part = (float*)((char*)ws + align_up(items * V.hkv * 16 * NT * (int64_t)sizeof(Partial), 256));
-  const dim3 grid((unsigned)items, (unsigned)V.hkv);
+  float* part = (float*)((char*)ws + align_up(rows * (int64_t)sizeof(Partial), 256));
+  const dim3 grid((unsigned)(one ? (a.total < V.n_seqs ? a.total : V.n_seqs) : sp.want), (unsigned)V.hkv);
   const auto kernel = V.code == HCA_E4M3 ? paged_rows_kernel<D, NT, true> : paged_rows_kernel<D, NT, false>;
   if (lds > 65536) {
     static std::atomic<uint64_t> done[2];
@@ -918,7 +916,7 @@ size_t hca_paged_workspace_bytes(const hca_paged_shape* shape, int64_t total_q, 
   PagedView V;
   if (paged_view(shape, &V) != HCA_OK || total_q < 0 || max_q < 0) return 0;
   if (max_q > total_q) max_q = (int32_t)total_q;
-  const int64_t rows = rows_items(V, total_q) * V.hkv * rows_cols(V, max_q);
+  const int64_t rows = 2 * (int64_t)rows_want(V) * V.hkv * rows_cols(V, max_q);
   return (size_t)(align_up(rows * (int64_t)sizeof(Partial), 256) + align_up(rows * V.D * 4, 256) + 256);
 }
 

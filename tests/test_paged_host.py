@@ -31,7 +31,8 @@ def test_buffer_sizes_follow_the_layout(B):
 
 BAD = [(dict(n_seqs=0), -1), (dict(n_q_heads=30), -1), (dict(n_pages=0), -1), (dict(max_pages=0), -1), (dict(n_kv_heads=0), -1),
        (dict(n_seqs=1025), -2), (dict(page=48), -2), (dict(page=8), -2), (dict(page=256), -2), (dict(head_dim=96), -2),
-       (dict(head_dim=256), -2), (dict(n_q_heads=136), -2), (dict(n_pages=2 ** 25), -2), (dict(max_pages=2 ** 24 + 1), -2)]
+       (dict(head_dim=256), -2), (dict(n_q_heads=136), -2), (dict(n_pages=2 ** 25), -2), (dict(max_pages=2 ** 24 + 1), -2),
+       (dict(n_seqs=1024, max_pages=2 ** 21 + 1), -2)]
 
 
 @pytest.mark.parametrize("kw,code", BAD)
