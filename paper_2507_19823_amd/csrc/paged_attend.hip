@@ -58,6 +58,104 @@ __device__ __forceinline__ float rows_sum(float x) {
   return __uint_as_float(r32[0]) + __uint_as_float(r32[1]);
 }
 
+// A tile of open rows (16 numbers per lane and 64 channels, as stored) as halves, brought into their range by a power of two:
+// bfloat16 keys to the top of it (below that nothing is lost that counts), values to that of codes, so that their weights
+// are no smaller than a whole page's.  Rows from token n on may hold anything: a key row stays in its own column of the
+// scores, which is masked, so it only must not decide the power; value rows are cleared.  Returns the exponent.
+template <int NH, bool BF16>
+__device__ __forceinline__ int open_keys(const uint4 (&raw)[NH][2], bool live, h8 (&o)[NH][2]) {
+  if (!BF16) {
+#pragma unroll
+    for (int x = 0; x < NH; ++x)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) o[x][e] = __builtin_bit_cast(h8, raw[x][e]);
+    return 0;
+  }
+  float amax = 0.f;
+#pragma unroll
+  for (int x = 0; x < NH; ++x)
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        amax = fmaxf(amax, fmaxf(fabsf(elem_to_float<true>(word(raw[x][e], i) & 0xffffu)), fabsf(elem_to_float<true>(word(raw[x][e], i) >> 16))));
+  amax = wave_max(live ? amax : 0.f);
+  int ex = amax > 0.f ? 14 - ilogbf(amax) : 0;
+  ex = ex > 64 ? 64 : ex;
+  const float up = ldexpf(1.0f, ex);
+#pragma unroll
+  for (int x = 0; x < NH; ++x)
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        o[x][e][2 * i] = (_Float16)(elem_to_float<true>(word(raw[x][e], i) & 0xffffu) * up);
+        o[x][e][2 * i + 1] = (_Float16)(elem_to_float<true>(word(raw[x][e], i) >> 16) * up);
+      }
+  return ex;
+}
+// first: the token of the lane's numbers 0, 4, 8 and 12 (the others follow it)
+template <int NH, bool BF16>
+__device__ __forceinline__ int open_values(uint4 (&raw)[NH][2], int first, int n, h8 (&o)[NH][2]) {
+  uint32_t keep[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) keep[i] = (first + 2 * i < n ? 0xffffu : 0u) | (first + 2 * i + 1 < n ? 0xffff0000u : 0u);
+  uint32_t top = 0;                                     // magnitudes are ordered like their bits
+#pragma unroll
+  for (int x = 0; x < NH; ++x)
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      uint32_t wd[4] = {raw[x][e].x & keep[0], raw[x][e].y & keep[1], raw[x][e].z & keep[0], raw[x][e].w & keep[1]};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t hi = wd[i] >> 16 & 0x7fffu, lo = wd[i] & 0x7fffu;
+        top = hi > top ? hi : top;
+        top = lo > top ? lo : top;
+      }
+      raw[x][e] = uint4{wd[0], wd[1], wd[2], wd[3]};
+    }
+  const float amax = elem_to_float<BF16>(wave_max(top));
+  int ex = amax > 0.f ? 6 - ilogbf(amax) : 0;
+  ex = ex > 64 ? 64 : ex;
+  const float up = ldexpf(1.0f, ex);
+#pragma unroll
+  for (int x = 0; x < NH; ++x)
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        o[x][e][2 * i] = (_Float16)(elem_to_float<BF16>(word(raw[x][e], i) & 0xffffu) * up);
+        o[x][e][2 * i + 1] = (_Float16)(elem_to_float<BF16>(word(raw[x][e], i) >> 16) * up);
+      }
+    }
+  return ex;
+}
+// Halves of a query row's 8 numbers, given in bfloat16 times a power of two.
+__device__ __forceinline__ h8 query_halves(const uint4& raw, float up) {
+  h8 o;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    o[2 * i] = (_Float16)(elem_to_float<true>(word(raw, i) & 0xffffu) * up);
+    o[2 * i + 1] = (_Float16)(elem_to_float<true>(word(raw, i) >> 16) * up);
+  }
+  return o;
+}
+// ... of which the largest of the row gets 2^14 .. 2^15
+__device__ __forceinline__ int query_exponent(float amax) {
+  const int ex = amax > 0.f ? 14 - ilogbf(amax) : 0;
+  return ex > 100 ? 100 : ex;
+}
+__device__ __forceinline__ float largest(const uint4& raw) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t hi = word(raw, i) >> 16 & 0x7fffu, lo = word(raw, i) & 0x7fffu;
+    top = hi > top ? hi : top;
+    top = lo > top ? lo : top;
+  }
+  return elem_to_float<true>(top);
+}
+
 // ---- few query rows: the cache is read once, at the rate of the memory ------------------------------
 // All query rows of a sequence that share a KV head (queries x heads of the group, up to 16 NT of them) are the columns of one
 // matrix product, so a token's codes are loaded and converted once.  Scores are computed transposed, S^T = K Q^T: then the
@@ -95,6 +193,19 @@ __device__ __forceinline__ int seq_units(const PagedView& V, const AttendArgs& a
   const int u = ((seq_len(V, a, b) >> V.lp << V.lp) + kUnit - 1) / kUnit;
   return u > 1 ? u : 1;
 }
+struct Seq { int row0, m, n, units; };                 // first query row, queries, tokens, units
+__device__ __forceinline__ Seq seq_info(const PagedView& V, const AttendArgs& a, int b) {
+  Seq s;
+  s.n = seq_len(V, a, b);
+  s.m = paged_rows(a.cu, b, a.total, &s.row0);
+  const int u = ((s.n >> V.lp << V.lp) + kUnit - 1) / kUnit;
+  s.units = s.m == 0 ? 0 : u > 1 ? u : 1;
+  return s;
+}
+__device__ __forceinline__ Seq seq_of_lane(const Seq& s, int l) {
+  return Seq{__builtin_amdgcn_readlane(s.row0, l), __builtin_amdgcn_readlane(s.m, l), __builtin_amdgcn_readlane(s.n, l),
+             __builtin_amdgcn_readlane(s.units, l)};
+}
 // units per workgroup (all units together are fewer than 2^31: see paged_view)
 __device__ __forceinline__ int split_len(const SplitPlan& sp, uint32_t all) {
   const int C = (int)((all + (uint32_t)sp.want - 1) / (uint32_t)sp.want);
@@ -107,12 +218,12 @@ __device__ __forceinline__ uint32_t all_units(const PagedView& V, const AttendAr
 }
 
 // Four channels of output row `at` from the weighted values, the reference and the sum of the weights.
-template <int D>
+template <int D, bool BF16>
 __device__ __forceinline__ void write_row(const PagedView& V, const AttendArgs& a, int64_t at, int ch, f4 o, float M, float sum) {
   const float inv = sum > 0.f ? 1.0f / sum : 0.f;
   uint16_t u[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) u[i] = V.elem == HCA_BF16 ? float_to_elem<true>(o[i] * inv) : float_to_elem<false>(o[i] * inv);
+  for (int i = 0; i < 4; ++i) u[i] = float_to_elem<BF16>(o[i] * inv);
   *reinterpret_cast<uint2*>(a.y + at * D + ch) = uint2{u[0] | (uint32_t)u[1] << 16, u[2] | (uint32_t)u[3] << 16};
   if (ch == 0 && a.lse != nullptr) a.lse[at] = sum > 0.f ? (M + log2f(sum)) * 0.693147180559945309f : -INFINITY;
 }
@@ -121,7 +232,7 @@ struct Partial {          // of one item, KV head and row: reference, sum; the w
   float M, l;
 };
 
-template <int D, int NT, bool E4M3>
+template <int D, int NT, bool BF16, bool E4M3>
 __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void paged_rows_kernel(PagedView V, AttendArgs a, SplitPlan sp,
                                                                           Partial* __restrict__ ml, float* __restrict__ part) {
   constexpr int NH = D / 64, NC = D / 16, COLS = 16 * NT;
@@ -132,28 +243,45 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void paged_rows_kernel(PagedV
   const int h = blockIdx.y, G = V.gqa;
   const int64_t side = V.side();
 
-  // the workgroup's piece: from unit u of sequence b on, `left` units
+  // the workgroup's piece: from unit u of sequence b on, `left` units.  Up to 64 sequences: their lengths are read once.
   int b, u, left;
-  if (sp.want == 0) {
-    b = paged_find(V.n_seqs, blockIdx.x, &u, [&](int s) { return seq_units(V, a, s) > 0 ? 1 : 0; });
-    if (b >= V.n_seqs) return;
-    left = seq_units(V, a, b);
-  } else {
-    const uint32_t all = all_units(V, a);
-    const int C = split_len(sp, all);
+  Seq sq;
+  const auto whole_seqs = [&](int units) { return sp.want == 0 ? (units > 0 ? 1 : 0) : units; };
+  if (V.n_seqs <= 64) {
+    Seq mine{0, 0, 0, 0};
+    if (lane < V.n_seqs) mine = seq_info(V, a, lane);
+    const int c = whole_seqs(mine.units);
+    const uint32_t incl = wave_scan_incl((uint32_t)c), all = wave_last(incl);
+    const int C = sp.want == 0 ? 1 : split_len(sp, all);
     const int64_t U0 = (int64_t)blockIdx.x * C;
     if (U0 >= all) return;
     left = all - U0 < C ? (int)(all - U0) : C;
-    b = paged_find(V.n_seqs, (int)U0, &u, [&](int s) { return seq_units(V, a, s); });
+    const int l = __builtin_ctzll(__ballot(incl > (uint32_t)U0));
+    b = l;
+    u = (int)U0 - (__builtin_amdgcn_readlane((int)incl, l) - __builtin_amdgcn_readlane(c, l));
+    sq = seq_of_lane(mine, l);
+  } else {
+    int C = 1;
+    uint32_t all = 0xffffffffu;
+    if (sp.want != 0) {
+      all = all_units(V, a);
+      C = split_len(sp, all);
+    }
+    const int64_t U0 = (int64_t)blockIdx.x * C;
+    if (U0 >= all) return;
+    left = all - U0 < C ? (int)(all - U0) : C;
+    b = paged_find(V.n_seqs, (int)U0, &u, [&](int x) { return whole_seqs(seq_units(V, a, x)); });
+    if (b >= V.n_seqs) return;
+    sq = seq_info(V, a, b);
   }
+  if (sp.want == 0) left = sq.units;
 
   for (bool first = true;; first = false) {
-    const int units = seq_units(V, a, b);
+    const int units = sq.units;
     const int ue = units - u < left ? units : u + left;
-    int row0;
-    const int m_all = paged_rows(a.cu, b, a.total, &row0);
+    const int row0 = sq.row0, m_all = sq.m;
     const int m = m_all < a.max_q ? m_all : a.max_q;
-    const int n = seq_len(V, a, b), whole = n >> V.lp << V.lp;
+    const int n = sq.n, whole = n >> V.lp << V.lp;
     const int R = m * G;                               // rows in use
 
     // whole pages: steps of STEP tokens, wave w takes every fourth
@@ -195,35 +323,21 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void paged_rows_kernel(PagedV
         for (int e = 0; e < 2; ++e)
           raw[x][e] = live ? *reinterpret_cast<const uint4*>(qp + 64 * x + 16 * g + 8 * e) : uint4{0, 0, 0, 0};
       qs[nt] = a.sm;
-      if (V.elem == HCA_BF16) {
+      float up = 1.f;
+      if (BF16) {
         float amax = 0.f;
 #pragma unroll
         for (int x = 0; x < NH; ++x)
 #pragma unroll
-          for (int e = 0; e < 2; ++e)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-              amax = fmaxf(amax, fmaxf(fabsf(elem_to_float<true>(word(raw[x][e], i) & 0xffffu)), fabsf(elem_to_float<true>(word(raw[x][e], i) >> 16))));
-        amax = rows_max(amax);
-        int ex = amax > 0.f ? 14 - ilogbf(amax) : 0;
-        ex = ex > 100 ? 100 : ex;                      // largest magnitude in [2^14, 2^15)
-        const float up = ldexpf(1.0f, ex);
+          for (int e = 0; e < 2; ++e) amax = fmaxf(amax, largest(raw[x][e]));
+        const int ex = query_exponent(rows_max(amax));
+        up = ldexpf(1.0f, ex);
         qs[nt] = ldexpf(a.sm, -ex);
-#pragma unroll
-        for (int x = 0; x < NH; ++x)
-#pragma unroll
-          for (int e = 0; e < 2; ++e)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              q[nt][x][e][2 * i] = (_Float16)(elem_to_float<true>(word(raw[x][e], i) & 0xffffu) * up);
-              q[nt][x][e][2 * i + 1] = (_Float16)(elem_to_float<true>(word(raw[x][e], i) >> 16) * up);
-            }
-      } else {
-#pragma unroll
-        for (int x = 0; x < NH; ++x)
-#pragma unroll
-          for (int e = 0; e < 2; ++e) q[nt][x][e] = __builtin_bit_cast(h8, raw[x][e]);
       }
+#pragma unroll
+      for (int x = 0; x < NH; ++x)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) q[nt][x][e] = BF16 ? query_halves(raw[x][e], up) : __builtin_bit_cast(h8, raw[x][e]);
     }
     least_seen = (int)wave_min((uint32_t)least_seen);
 
@@ -308,6 +422,46 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void paged_rows_kernel(PagedV
       load(0, vw, side);
       sc = ask_scale(id);
     }
+    // open rows, a tile at a time, where the piece ends the sequence: the same with halves made from the rows themselves, while
+    // the first codes are on their way; by the waves that have the fewest steps
+    if (ue == units) {
+      for (int t0 = whole + 16 * (3 - w); t0 < n; t0 += 64) {
+        const uint16_t* kp = a.open + ((int64_t)b * V.hkv + h) * 2 * side + (t0 & (V.P - 1)) * D;
+        uint4 raw[2][NH][2];
+#pragma unroll
+        for (int sd = 0; sd < 2; ++sd)
+#pragma unroll
+          for (int x = 0; x < NH; ++x)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) raw[sd][x][e] = *(reinterpret_cast<const uint4*>(kp + sd * side + (x * 64 + lane) * 16) + e);
+        h8 o[NH][2];
+        const float ks = ldexpf(1.0f, -open_keys<NH, BF16>(raw[0], t0 + l16 < n, o));
+        f4 s[NT][1];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          s[nt][0] = f4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int x = 0; x < NH; ++x)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) s[nt][0] = __builtin_amdgcn_mfma_f32_16x16x32_f16(o[x][e], q[nt][x][e], s[nt][0], 0, 0, 0);
+        }
+        const int ex = open_values<NH, BF16>(raw[1], t0 + 4 * g, n, o);
+        const float lv = (float)-ex, iv = ldexpf(1.0f, ex);
+        h2 p[NT][1][2];
+        weigh(std::integral_constant<int, 1>{}, s, &ks, &lv, &iv, t0, n, p);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          const h4 pb = h4{p[nt][0][0].x, p[nt][0][0].y, p[nt][0][1].x, p[nt][0][1].y};
+#pragma unroll
+          for (int c = 0; c < NC; ++c) {               // channels 16 c + l16: numbers 4 (c % 4) .. + 3 of the lane's sixteen
+            const h8 v = o[c >> 2][(c & 3) >> 1];
+            const int z = 4 * (c & 1);
+            y[nt][c] = __builtin_amdgcn_mfma_f32_16x16x16f16(h4{v[z], v[z + 1], v[z + 2], v[z + 3]}, pb, y[nt][c], 0, 0, 0);
+          }
+        }
+      }
+    }
+
     float sc_lv = log2_raw(sc.y), sc_iv = 1.0f / sc.y;
     for (int k = 0; k < nk; ++k) {
       const int kg = k % group;
@@ -365,78 +519,6 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void paged_rows_kernel(PagedV
       if (more) load(k + 1, vw, side);
     }
 
-    // open rows, a tile at a time, where the piece ends the sequence: the same with halves made from the rows themselves
-    if (ue == units) {
-      const auto widen = [&](uint32_t bits) { return V.elem == HCA_BF16 ? elem_to_float<true>(bits) : elem_to_float<false>(bits); };
-      for (int t0 = whole + 16 * w; t0 < n; t0 += 64) {
-        const uint16_t* kp = a.open + ((int64_t)b * V.hkv + h) * 2 * side + (t0 & (V.P - 1)) * D;
-        float ks, lv, iv;
-        f4 s[NT][1];
-        h2 p[NT][1][2];
-#pragma unroll
-        for (int sd = 0; sd < 2; ++sd) {
-          uint4 raw[NH][2];
-          float amax = 0.f;
-#pragma unroll
-          for (int x = 0; x < NH; ++x)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              const uint4 v = *(reinterpret_cast<const uint4*>(kp + sd * side + (x * 64 + lane) * 16) + e);
-              // rows behind the last token may hold anything: keys by lane, values by place in the tile
-              uint32_t wd[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                const int a0 = sd == 0 ? t0 + l16 : t0 + 4 * g + 2 * (i & 1), a1 = sd == 0 ? t0 + l16 : a0 + 1;
-                wd[i] = (a0 < n ? wd[i] & 0xffffu : 0u) | (a1 < n ? wd[i] & 0xffff0000u : 0u);
-                amax = fmaxf(amax, fmaxf(fabsf(widen(wd[i] & 0xffffu)), fabsf(widen(wd[i] >> 16))));
-              }
-              raw[x][e] = uint4{wd[0], wd[1], wd[2], wd[3]};
-            }
-          // a power of two brings them to the halves' range: bfloat16 keys to the top of it (below it nothing is lost
-          // that counts), values to that of codes, so that their weights are no smaller than a whole page's
-          amax = wave_max(amax);
-          int ex = amax > 0.f && (sd == 1 || V.elem == HCA_BF16) ? (sd == 0 ? 14 : 6) - ilogbf(amax) : 0;
-          ex = ex > 64 ? 64 : ex;
-          const float up = ldexpf(1.0f, ex);
-          h8 o[NH][2];
-#pragma unroll
-          for (int x = 0; x < NH; ++x)
-#pragma unroll
-            for (int e = 0; e < 2; ++e)
-#pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                o[x][e][2 * i] = (_Float16)(widen(word(raw[x][e], i) & 0xffffu) * up);
-                o[x][e][2 * i + 1] = (_Float16)(widen(word(raw[x][e], i) >> 16) * up);
-              }
-          if (sd == 0) {
-            ks = ldexpf(1.0f, -ex);
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-              s[nt][0] = f4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-              for (int x = 0; x < NH; ++x)
-#pragma unroll
-                for (int e = 0; e < 2; ++e) s[nt][0] = __builtin_amdgcn_mfma_f32_16x16x32_f16(o[x][e], q[nt][x][e], s[nt][0], 0, 0, 0);
-            }
-          } else {
-            lv = (float)-ex;
-            iv = up;
-            weigh(std::integral_constant<int, 1>{}, s, &ks, &lv, &iv, t0, n, p);
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-              const h4 pb = h4{p[nt][0][0].x, p[nt][0][0].y, p[nt][0][1].x, p[nt][0][1].y};
-#pragma unroll
-              for (int c = 0; c < NC; ++c) {           // channels 16 c + l16: numbers 4 (c % 4) .. + 3 of the lane's sixteen
-                const h8 v = o[c >> 2][(c & 3) >> 1];
-                const int z = 4 * (c & 1);
-                y[nt][c] = __builtin_amdgcn_mfma_f32_16x16x16f16(h4{v[z], v[z + 1], v[z + 2], v[z + 3]}, pb, y[nt][c], 0, 0, 0);
-              }
-            }
-          }
-        }
-      }
-    }
-
     // the four waves' results are joined
     constexpr int RS = D + 4;
     float* sM = lds + 4 * COLS * RS;
@@ -467,7 +549,7 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void paged_rows_kernel(PagedV
         o += *reinterpret_cast<const f4*>(lds + (x * COLS + r) * RS + ch) * f;
       }
       if (only) {
-        write_row<D>(V, a, (int64_t)(row0 + r / G) * V.hq + h * G + r % G, ch, o, top, sum);
+        write_row<D, BF16>(V, a, (int64_t)(row0 + r / G) * V.hq + h * G + r % G, ch, o, top, sum);
       } else {
         const int64_t at = ((2 * (int64_t)blockIdx.x + (first ? 0 : 1)) * V.hkv + h) * COLS + r;
         *reinterpret_cast<f4*>(part + at * D + ch) = o;
@@ -476,62 +558,95 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void paged_rows_kernel(PagedV
     }
     left -= ue - u;
     if (left <= 0) return;
-    do ++b; while (b < V.n_seqs && seq_units(V, a, b) == 0);
-    if (b >= V.n_seqs) return;
+    do {
+      if (++b >= V.n_seqs) return;
+      sq = seq_info(V, a, b);
+    } while (sq.units == 0);
     u = 0;
     __syncthreads();                                    // LDS is free again
   }
 }
 
-// Joins the pieces of sequences that have several.  One workgroup per query row and head, pieces in a fixed order.
+// Joins the pieces of sequences that have several.  One workgroup per query row and head, pieces in a fixed order.  A few KB
+// of reading that wait for one another: lengths, then the pieces' references, sums and values at once (each group of threads
+// keeps a running reference of its own), then the output.
 template <int D>
 __global__ __launch_bounds__(256) void paged_join_kernel(PagedView V, AttendArgs a, SplitPlan sp, int cols, const Partial* __restrict__ ml,
                                                          const float* __restrict__ part) {
   constexpr int TPR = D / 4, NG = 256 / TPR;            // groups of threads, each with every NG-th piece
   __shared__ f4 s_o[NG][TPR];
-  __shared__ float s_l[NG];
-  const int hq = blockIdx.y, h = hq / V.gqa, lane = threadIdx.x & 63;
-  int i;
-  const int b = paged_find(V.n_seqs, blockIdx.x, &i, [&](int s) { int f; return paged_rows(a.cu, s, a.total, &f); });
-  if (b >= V.n_seqs || i >= a.max_q) return;
-  uint32_t all = 0, before = 0;
-  for (int s = lane; s < V.n_seqs; s += 64) {
-    const uint32_t c = (uint32_t)seq_units(V, a, s);
-    all += c;
-    before += s < b ? c : 0;
+  __shared__ Partial s_ml[NG];
+  const int hq = blockIdx.y, h = hq / V.gqa, lane = threadIdx.x & 63, t = blockIdx.x;
+  // the row's sequence b, query i, and the units before and in it
+  int b = -1, i = 0, S = 0, E = 0;
+  uint32_t all = 0;
+  for (int b0 = 0; b0 < V.n_seqs; b0 += 64) {
+    const int s = b0 + lane;
+    int f = 0, m = 0;
+    uint32_t c = 0;
+    if (s < V.n_seqs) {
+      m = paged_rows(a.cu, s, a.total, &f);
+      c = (uint32_t)seq_units(V, a, s);
+    }
+    const uint32_t incl = wave_scan_incl(c);
+    const uint64_t mine = __ballot(m > 0 && t >= f && t < f + m);
+    if (b < 0 && mine != 0) {
+      const int l = __builtin_ctzll(mine);
+      b = b0 + l;
+      i = t - __builtin_amdgcn_readlane(f, l);
+      E = (int)(all + (uint32_t)__builtin_amdgcn_readlane((int)incl, l));
+      S = E - __builtin_amdgcn_readlane((int)c, l);
+    }
+    all += wave_last(incl);
   }
-  const int C = split_len(sp, wave_sum(all));
-  const int S = (int)wave_sum(before), E = S + seq_units(V, a, b);       // the sequence's units
+  if (b < 0 || i >= a.max_q) return;
+  const int C = split_len(sp, all);
   const int i0 = S / C, count = (E - 1) / C - i0 + 1;                    // its workgroups
   if (count <= 1) return;
-  int row0;
-  (void)paged_rows(a.cu, b, a.total, &row0);
   const int r = i * V.gqa + hq % V.gqa;
   const int grp = threadIdx.x / TPR, ch = threadIdx.x % TPR * 4;
   const int late = S > i0 * C ? 1 : 0;                                   // the first piece is not its workgroup's first
   const auto at = [&](int k) { return ((2 * (int64_t)(i0 + k) + (k == 0 ? late : 0)) * V.hkv + h) * cols + r; };
-  float M = -1e30f;
-  for (int k = lane; k < count; k += 64) M = fmaxf(M, ml[at(k)].M);
-  M = wave_max(M);
-  float sum = 0.f;
+  float M = -1e30f, sum = 0.f;
   f4 o = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-  for (int k = grp; k < count; k += NG) {
-    const Partial p = ml[at(k)];
-    const float f = exp2_raw(p.M - M);
-    sum = fmaf(p.l, f, sum);
-    o += *reinterpret_cast<const f4*>(part + at(k) * D + ch) * f;
+  for (int k0 = grp; k0 < count; k0 += 4 * NG) {
+    Partial p[4];
+    f4 v[4];
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      const int64_t z = at(k0 + x * NG < count ? k0 + x * NG : k0);
+      p[x] = ml[z];
+      v[x] = *reinterpret_cast<const f4*>(part + z * D + ch);
+      if (k0 + x * NG >= count) p[x] = Partial{-1e30f, 0.f}, v[x] = f4{0.f, 0.f, 0.f, 0.f};
+    }
+    const float next = fmaxf(fmaxf(M, fmaxf(p[0].M, p[1].M)), fmaxf(p[2].M, p[3].M)), f0 = exp2_raw(M - next);
+    sum *= f0;
+    o *= f0;
+    M = next;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      const float f = exp2_raw(p[x].M - M);
+      sum = fmaf(p[x].l, f, sum);
+      o += v[x] * f;
+    }
   }
   s_o[grp][ch / 4] = o;
-  if (ch == 0) s_l[grp] = sum;
+  if (ch == 0) s_ml[grp] = Partial{M, sum};
   __syncthreads();
   if (grp != 0) return;
+  for (int x = 0; x < NG; ++x) M = fmaxf(M, s_ml[x].M);
+  sum = 0.f;
+  o = f4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-  for (int x = 1; x < NG; ++x) {
-    o += s_o[x][ch / 4];
-    sum += s_l[x];
+  for (int x = 0; x < NG; ++x) {
+    const float f = exp2_raw(s_ml[x].M - M);
+    sum = fmaf(s_ml[x].l, f, sum);
+    o += s_o[x][ch / 4] * f;
   }
-  write_row<D>(V, a, (int64_t)(row0 + i) * V.hq + hq, ch, o, M, sum);
+  if (V.elem == HCA_BF16)
+    write_row<D, true>(V, a, (int64_t)t * V.hq + hq, ch, o, M, sum);
+  else
+    write_row<D, false>(V, a, (int64_t)t * V.hq + hq, ch, o, M, sum);
 }
 
 // ---- many query rows: the matrix cores are the bound -------------------------------------------------
@@ -560,7 +675,7 @@ __device__ __forceinline__ int seq_rows(const PagedView& V, const AttendArgs& a,
   return (m < a.max_q ? m : a.max_q) * V.gqa;
 }
 
-template <int D, bool E4M3>
+template <int D, bool BF16, bool E4M3>
 __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedView V, AttendArgs a) {
   constexpr int NH = D / 64, NS = D / 16, NC = D / 32, NW = 4, ROWS = 32 * NW;
   extern __shared__ char lds_raw[];
@@ -594,31 +709,19 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedView V, AttendA
   {
     const uint16_t* qp = a.q + (int64_t)(row0 + qi) * a.q_stride + (int64_t)hq * D;
     uint4 raw[NS];
-    float amax = 0.f;
 #pragma unroll
-    for (int s = 0; s < NS; ++s) {
-      raw[s] = live ? *reinterpret_cast<const uint4*>(qp + 16 * s + 8 * hh) : uint4{0, 0, 0, 0};
+    for (int s = 0; s < NS; ++s) raw[s] = live ? *reinterpret_cast<const uint4*>(qp + 16 * s + 8 * hh) : uint4{0, 0, 0, 0};
+    float up = 1.f;
+    if (BF16) {
+      float amax = 0.f;
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        amax = fmaxf(amax, fmaxf(fabsf(elem_to_float<true>(word(raw[s], i) & 0xffffu)), fabsf(elem_to_float<true>(word(raw[s], i) >> 16))));
-    }
-    if (V.elem == HCA_BF16) {
-      amax = halves_max(amax);
-      int ex = amax > 0.f ? 14 - ilogbf(amax) : 0;
-      ex = ex > 100 ? 100 : ex;
-      const float up = ldexpf(1.0f, ex);
+      for (int s = 0; s < NS; ++s) amax = fmaxf(amax, largest(raw[s]));
+      const int ex = query_exponent(halves_max(amax));
+      up = ldexpf(1.0f, ex);
       qs = ldexpf(a.sm, -ex);
-#pragma unroll
-      for (int s = 0; s < NS; ++s)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          q[s][2 * i] = (_Float16)(elem_to_float<true>(word(raw[s], i) & 0xffffu) * up);
-          q[s][2 * i + 1] = (_Float16)(elem_to_float<true>(word(raw[s], i) >> 16) * up);
-        }
-    } else {
-#pragma unroll
-      for (int s = 0; s < NS; ++s) q[s] = __builtin_bit_cast(h8, raw[s]);
     }
+#pragma unroll
+    for (int s = 0; s < NS; ++s) q[s] = BF16 ? query_halves(raw[s], up) : __builtin_bit_cast(h8, raw[s]);
   }
   const int least_seen = (int)wave_min((uint32_t)sees), most_seen = (int)wave_max((uint32_t)sees);
   const int r_last = rt * ROWS + ROWS - 1 < R ? rt * ROWS + ROWS - 1 : R - 1;
@@ -690,52 +793,31 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedView V, AttendA
         }
     } else if (t >= whole && t < n) {                            // open rows: scaled by powers of two, as above
       const uint16_t* kp = a.open + ((int64_t)b * V.hkv + h) * 2 * side + (t & (V.P - 1)) * D;
-      int ex[2];
+      uint4 raw[2][NH][2];
 #pragma unroll
-      for (int sd = 0; sd < 2; ++sd) {
-        uint4 raw[NH][2];
-        float amax = 0.f;
-        const auto widen = [&](uint32_t bits) { return V.elem == HCA_BF16 ? elem_to_float<true>(bits) : elem_to_float<false>(bits); };
+      for (int sd = 0; sd < 2; ++sd)
 #pragma unroll
         for (int z = 0; z < NH; ++z)
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const uint4 v = *(reinterpret_cast<const uint4*>(kp + sd * side + (z * 64 + lane) * 16) + e);
-            uint32_t wd[4] = {v.x, v.y, v.z, v.w};
+          for (int e = 0; e < 2; ++e) raw[sd][z][e] = *(reinterpret_cast<const uint4*>(kp + sd * side + (z * 64 + lane) * 16) + e);
+      h8 o[NH][2];
+      const int kx = open_keys<NH, BF16>(raw[0], t + l16 < n, o);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const int a0 = sd == 0 ? t + l16 : t + 4 * g + 2 * (i & 1), a1 = sd == 0 ? t + l16 : a0 + 1;
-              wd[i] = (a0 < n ? wd[i] & 0xffffu : 0u) | (a1 < n ? wd[i] & 0xffff0000u : 0u);
-              amax = fmaxf(amax, fmaxf(fabsf(widen(wd[i] & 0xffffu)), fabsf(widen(wd[i] >> 16))));
-            }
-            raw[z][e] = uint4{wd[0], wd[1], wd[2], wd[3]};
-          }
-        amax = wave_max(amax);
-        ex[sd] = amax > 0.f && (sd == 1 || V.elem == HCA_BF16) ? (sd == 0 ? 14 : 6) - ilogbf(amax) : 0;
-        ex[sd] = ex[sd] > 64 ? 64 : ex[sd];
-        const float up = ldexpf(1.0f, ex[sd]);
+      for (int z = 0; z < NH; ++z)
 #pragma unroll
-        for (int z = 0; z < NH; ++z)
+        for (int e = 0; e < 2; ++e) put_key(buf, z, e, o[z][e]);
+      const int vx = open_values<NH, BF16>(raw[1], t + 4 * g, n, o);
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            h8 o;
+      for (int z = 0; z < NH; ++z)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const uint32_t x = word(raw[z][e], i);
-              o[2 * i] = (_Float16)(widen(x & 0xffffu) * up);
-              o[2 * i + 1] = (_Float16)(widen(x >> 16) * up);
-            }
-            if (sd == 0) {
-              put_key(buf, z, e, o);
-            } else {
-              put_value(buf, z, 2 * e, h2{o[0], o[1]}, h2{o[2], o[3]});
-              put_value(buf, z, 2 * e + 1, h2{o[4], o[5]}, h2{o[6], o[7]});
-            }
-          }
-      }
-      ks = ldexpf(1.0f, -ex[0]);
-      lv = (float)-ex[1];
-      iv = ldexpf(1.0f, ex[1]);
+        for (int e = 0; e < 2; ++e) {
+          const h8 v = o[z][e];
+          put_value(buf, z, 2 * e, h2{v[0], v[1]}, h2{v[2], v[3]});
+          put_value(buf, z, 2 * e + 1, h2{v[4], v[5]}, h2{v[6], v[7]});
+        }
+      ks = ldexpf(1.0f, -kx);
+      lv = (float)-vx;
+      iv = ldexpf(1.0f, vx);
     } else {                                                     // no tokens: zeros, and no weight
       const h8 zero = {0, 0, 0, 0, 0, 0, 0, 0};
       const h2 none = {0, 0};
@@ -844,7 +926,7 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedView V, AttendA
     for (int i = 0; i < 16; i += 4) {
       uint16_t o[4];
 #pragma unroll
-      for (int x = 0; x < 4; ++x) o[x] = V.elem == HCA_BF16 ? float_to_elem<true>(y[c][i + x] * inv) : float_to_elem<false>(y[c][i + x] * inv);
+      for (int x = 0; x < 4; ++x) o[x] = float_to_elem<BF16>(y[c][i + x] * inv);
       *reinterpret_cast<uint2*>(a.y + at * D + 32 * c + 8 * (i >> 2) + 4 * hh) = uint2{o[0] | (uint32_t)o[1] << 16, o[2] | (uint32_t)o[3] << 16};
     }
   if (hh == 0 && a.lse != nullptr) a.lse[at] = l > 0.f ? (M + log2f(l)) * 0.693147180559945309f : -INFINITY;
@@ -854,10 +936,12 @@ template <int D>
 static int32_t launch_tiles(const PagedView& V, const AttendArgs& a, hipStream_t st) {
   constexpr int lds = 2 * 64 * D * 2 * 2 + 2 * 16 * 4;
   const int64_t tiles = (int64_t)a.total * V.gqa / 128 + (a.total < V.n_seqs ? a.total : V.n_seqs);
-  const auto kernel = V.code == HCA_E4M3 ? paged_tile_kernel<D, true> : paged_tile_kernel<D, false>;
+  const int which = (V.elem == HCA_BF16 ? 2 : 0) + (V.code == HCA_E4M3 ? 1 : 0);
+  const auto kernel = which == 0 ? paged_tile_kernel<D, false, false> : which == 1 ? paged_tile_kernel<D, false, true>
+                    : which == 2 ? paged_tile_kernel<D, true, false> : paged_tile_kernel<D, true, true>;
   if (lds > 65536) {
-    static std::atomic<uint64_t> done[2];
-    const int32_t rc = lds_opt_in((const void*)kernel, lds, &done[V.code == HCA_E4M3]);
+    static std::atomic<uint64_t> done[4];
+    const int32_t rc = lds_opt_in((const void*)kernel, lds, &done[which]);
     if (rc != HCA_OK) return rc;
   }
   kernel<<<(unsigned)(tiles * V.hkv), 256, lds, st>>>(V, a);
@@ -867,7 +951,7 @@ static int32_t launch_tiles(const PagedView& V, const AttendArgs& a, hipStream_t
 
 // Workgroups per KV head that fill the chip once: two on each of its 256 compute units.
 static int rows_want(const PagedView& V) { return V.hkv >= 512 ? 1 : 512 / V.hkv; }
-constexpr int kOneItem = 1024;      // sequences up to this length are one piece, and nothing has to be joined
+constexpr int kOneItem = 256;      // sequences up to this length are one piece, and nothing has to be joined
 
 static int rows_cols(const PagedView& V, int max_q) {
   const int64_t R = (int64_t)max_q * V.gqa;
@@ -883,10 +967,12 @@ static int32_t launch_rows_nt(const PagedView& V, const AttendArgs& a, int64_t m
   Partial* ml = (Partial*)ws;
   float* part = (float*)((char*)ws + align_up(rows * (int64_t)sizeof(Partial), 256));
   const dim3 grid((unsigned)(one ? (a.total < V.n_seqs ? a.total : V.n_seqs) : sp.want), (unsigned)V.hkv);
-  const auto kernel = V.code == HCA_E4M3 ? paged_rows_kernel<D, NT, true> : paged_rows_kernel<D, NT, false>;
+  const int which = (V.elem == HCA_BF16 ? 2 : 0) + (V.code == HCA_E4M3 ? 1 : 0);
+  const auto kernel = which == 0 ? paged_rows_kernel<D, NT, false, false> : which == 1 ? paged_rows_kernel<D, NT, false, true>
+                    : which == 2 ? paged_rows_kernel<D, NT, true, false> : paged_rows_kernel<D, NT, true, true>;
   if (lds > 65536) {
-    static std::atomic<uint64_t> done[2];
-    const int32_t rc = lds_opt_in((const void*)kernel, lds, &done[V.code == HCA_E4M3]);
+    static std::atomic<uint64_t> done[4];
+    const int32_t rc = lds_opt_in((const void*)kernel, lds, &done[which]);
     if (rc != HCA_OK) return rc;
   }
   kernel<<<grid, 256, lds, st>>>(V, a, sp, ml, part);
