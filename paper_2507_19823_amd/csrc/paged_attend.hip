@@ -233,7 +233,7 @@ struct Partial {          // of one item, KV head and row: reference, sum; the w
 };
 
 template <int D, int NT, bool BF16, bool E4M3>
-__global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void paged_rows_kernel(PagedView V, AttendArgs a, SplitPlan sp,
+__global__ __launch_bounds__(256, 2) void paged_rows_kernel(PagedView V, AttendArgs a, SplitPlan sp,
                                                                           Partial* __restrict__ ml, float* __restrict__ part) {
   constexpr int NH = D / 64, NC = D / 16, COLS = 16 * NT;
   constexpr int TT = NT == 1 ? 4 : 2, STEP = 16 * TT;  // tiles and tokens that a wave works on at a time
@@ -675,9 +675,48 @@ __device__ __forceinline__ int seq_rows(const PagedView& V, const AttendArgs& a,
   return (m < a.max_q ? m : a.max_q) * V.gqa;
 }
 
+// Where there are fewer tiles than the chip takes at once, the tokens are divided too: every tile of a sequence into ns
+// shares, ns from the sequence's units and L = all tiles' units / workgroups wanted.
+constexpr int kTileRows = 128;
+struct TilePlan {
+  int32_t want;         // workgroups per KV head to divide for; 0: a workgroup per tile
+  int32_t least;        // units per share at least
+};
+struct TileSeq { int tiles, units, ns; };
+__device__ __forceinline__ TileSeq tile_seq(const PagedView& V, const AttendArgs& a, int b) {
+  return TileSeq{(seq_rows(V, a, b) + kTileRows - 1) / kTileRows, (seq_len(V, a, b) + kUnit - 1) / kUnit, 1};
+}
+__device__ __forceinline__ int tile_len(const PagedView& V, const AttendArgs& a, const TilePlan& tp) {
+  uint64_t all = 0;
+  for (int b = threadIdx.x & 63; b < V.n_seqs; b += 64) {
+    const TileSeq t = tile_seq(V, a, b);
+    all += (uint64_t)t.tiles * (uint32_t)t.units;
+  }
+  all = wave_scan_incl(all);
+  all = (uint64_t)wave_last((uint32_t)(all >> 32)) << 32 | wave_last((uint32_t)all);
+  const uint64_t L = (all + (uint32_t)tp.want - 1) / (uint32_t)tp.want;
+  return L < (uint64_t)tp.least ? tp.least : L > 1u << 25 ? 1 << 25 : (int)L;
+}
+__device__ __forceinline__ TileSeq tile_shares(const PagedView& V, const AttendArgs& a, const TilePlan& tp, int L, int b) {
+  TileSeq t = tile_seq(V, a, b);
+  if (tp.want != 0 && t.units > L) t.ns = (t.units + L - 1) / L;
+  return t;
+}
+// the first place in the workspace of sequence b's shares: only divided sequences have any, and since a divided one has
+// ns <= 2 units / L, there are at most 2 want of them
+__device__ __forceinline__ int tile_places(const PagedView& V, const AttendArgs& a, const TilePlan& tp, int L, int b) {
+  uint32_t before = 0;
+  for (int s = threadIdx.x & 63; s < b; s += 64) {
+    const TileSeq t = tile_shares(V, a, tp, L, s);
+    before += t.ns > 1 ? (uint32_t)(t.tiles * t.ns) : 0;
+  }
+  return (int)wave_sum(before);
+}
+
 template <int D, bool BF16, bool E4M3>
-__global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedView V, AttendArgs a) {
-  constexpr int NH = D / 64, NS = D / 16, NC = D / 32, NW = 4, ROWS = 32 * NW;
+__global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedView V, AttendArgs a, TilePlan tp, Partial* __restrict__ ml,
+                                                            float* __restrict__ part) {
+  constexpr int NH = D / 64, NS = D / 16, NC = D / 32, ROWS = kTileRows;
   extern __shared__ char lds_raw[];
   h8* sk = reinterpret_cast<h8*>(lds_raw);                       // [2][D / 8][64]: 8 channels of a token
   h8* sv = sk + 2 * (D / 8) * 64;                                // [2][4][2][D]: 8 tokens of a channel
@@ -685,13 +724,18 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedView V, AttendA
   const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4, l32 = lane & 31, hh = lane >> 5;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int h = blockIdx.x % V.hkv;
+  const int L = tp.want == 0 ? 0 : tile_len(V, a, tp);
   int within;
-  const int b = paged_find(V.n_seqs, blockIdx.x / V.hkv, &within, [&](int s) { return (seq_rows(V, a, s) + ROWS - 1) / ROWS; });
+  const int b = paged_find(V.n_seqs, blockIdx.x / V.hkv, &within, [&](int s) {
+    const TileSeq t = tile_shares(V, a, tp, L, s);
+    return t.tiles * t.ns;
+  });
   if (b >= V.n_seqs) return;
+  const TileSeq ts = tile_shares(V, a, tp, L, b);
   int row0;
   const int m_all = paged_rows(a.cu, b, a.total, &row0);
   const int G = V.gqa, R = seq_rows(V, a, b);
-  const int rt = (R + ROWS - 1) / ROWS - 1 - within;             // the tiles that see most come first
+  const int rt = ts.tiles - 1 - within / ts.ns, share = within % ts.ns;      // the tiles that see most come first
   const int n = seq_len(V, a, b), whole = n >> V.lp << V.lp;
   const int64_t side = V.side();
 
@@ -723,9 +767,11 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedView V, AttendA
 #pragma unroll
     for (int s = 0; s < NS; ++s) q[s] = BF16 ? query_halves(raw[s], up) : __builtin_bit_cast(h8, raw[s]);
   }
-  const int least_seen = (int)wave_min((uint32_t)sees), most_seen = (int)wave_max((uint32_t)sees);
+  const int least_seen = (int)wave_min((uint32_t)sees);
+  const int most_seen = rt * ROWS + 32 * w < R ? (int)wave_max((uint32_t)sees) : 0;      // a wave without rows only loads
   const int r_last = rt * ROWS + ROWS - 1 < R ? rt * ROWS + ROWS - 1 : R - 1;
-  const int units = (seen(r_last / G) + kUnit - 1) / kUnit;      // of the workgroup
+  const int tile_units = (seen(r_last / G) + kUnit - 1) / kUnit;
+  const int u_begin = (int)((int64_t)tile_units * share / ts.ns), u_end = (int)((int64_t)tile_units * (share + 1) / ts.ns);
 
   float M = -1e30f, l = 0.f;
   f16v y[NC];
@@ -734,13 +780,13 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedView V, AttendA
 #pragma unroll
     for (int i = 0; i < 16; ++i) y[c][i] = 0.f;
 
-  // lane j holds the page of this wave's tile of unit base + j, and its scales
+  // lane j holds the page of this wave's tile of unit base + j (base every 64 units from u_begin on), and its scales
   const int32_t* table = a.tables + (int64_t)b * V.max_pages;
   struct Info { int id; float ks, vs; };
   const auto fetch = [&](int base) {
     const int t = (base + lane) * kUnit + 16 * w;
     Info f{-1, 0.f, 1.f};
-    if (t < whole && base + lane < units) {
+    if (t < whole && base + lane < u_end) {
       const int id = table[t >> V.lp];
       if (id >= 0 && id < V.n_pages) {
         const float2 sc = *reinterpret_cast<const float2*>(a.scale + ((int64_t)id * V.hkv + h) * 2);
@@ -749,15 +795,16 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedView V, AttendA
     }
     return f;
   };
-  Info pages = fetch(0);
+  Info pages = fetch(u_begin);
   uint4 kw[NH], vw[NH];
   float nks = 0.f, nvs = 1.f;
   int nid = -1;
   const auto load = [&](int u) {                                 // asks for the codes of this wave's tile of unit u
-    if ((u & 63) == 0 && u > 0) pages = fetch(u);
-    nid = __builtin_amdgcn_readlane(pages.id, u & 63);
-    nks = lane_value(pages.ks, u & 63);
-    nvs = lane_value(pages.vs, u & 63);
+    const int j = (u - u_begin) & 63;
+    if (j == 0 && u > u_begin) pages = fetch(u);
+    nid = __builtin_amdgcn_readlane(pages.id, j);
+    nks = lane_value(pages.ks, j);
+    nvs = lane_value(pages.vs, j);
     if (nid >= 0) {
       const int t = u * kUnit + 16 * w;
       const uint8_t* p = a.kv + ((int64_t)nid * V.hkv + h) * 2 * side + (t & (V.P - 1)) * D;
@@ -835,13 +882,13 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedView V, AttendA
     if (lane == 0) *reinterpret_cast<f4*>(sinfo + (buf * 4 + w) * 4) = f4{ks, lv, iv, 0.f};
   };
 
-  if (units > 0) {
-    load(0);
-    stage(0, 0);
-    if (units > 1) load(1);
+  if (u_begin < u_end) {
+    load(u_begin);
+    stage(u_begin, u_begin & 1);
+    if (u_begin + 1 < u_end) load(u_begin + 1);
   }
   __syncthreads();
-  for (int u = 0; u < units; ++u) {
+  for (int u = u_begin; u < u_end; ++u) {
     const int buf = u & 1, t0 = u * kUnit;
     if (t0 < most_seen) {
       f16v s[2];
@@ -909,14 +956,26 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedView V, AttendA
         for (int c = 0; c < NC; ++c)
           y[c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(sv[((buf * 4 + tt) * 2 + hh) * D + 32 * c + l32], p[tt], y[c], 0, 0, 0);
     }
-    if (u + 1 < units) {
+    if (u + 1 < u_end) {
       stage(u + 1, buf ^ 1);
-      if (u + 2 < units) load(u + 2);
+      if (u + 2 < u_end) load(u + 2);
     }
     __syncthreads();
   }
 
   l = halves_sum(l);
+  if (ts.ns > 1) {
+    const int place = tile_places(V, a, tp, L, b) + rt * ts.ns + share;
+    if (!live) return;
+    const int64_t z = ((int64_t)place * V.hkv + h) * kTileRows + 32 * w + l32;
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+      for (int i = 0; i < 16; i += 4)
+        *reinterpret_cast<f4*>(part + z * D + 32 * c + 8 * (i >> 2) + 4 * hh) = f4{y[c][i], y[c][i + 1], y[c][i + 2], y[c][i + 3]};
+    if (hh == 0) ml[z] = Partial{M, l};
+    return;
+  }
   if (!live) return;
   const int64_t at = (int64_t)(row0 + qi) * V.hq + hq;
   const float inv = l > 0.f ? 1.0f / l : 0.f;
@@ -932,31 +991,63 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedView V, AttendA
   if (hh == 0 && a.lse != nullptr) a.lse[at] = l > 0.f ? (M + log2f(l)) * 0.693147180559945309f : -INFINITY;
 }
 
+// Joins the shares of the tiles of divided sequences.  One workgroup per query and KV head.
 template <int D>
-static int32_t launch_tiles(const PagedView& V, const AttendArgs& a, hipStream_t st) {
-  constexpr int lds = 2 * 64 * D * 2 * 2 + 2 * 16 * 4;
-  const int64_t tiles = (int64_t)a.total * V.gqa / 128 + (a.total < V.n_seqs ? a.total : V.n_seqs);
-  const int which = (V.elem == HCA_BF16 ? 2 : 0) + (V.code == HCA_E4M3 ? 1 : 0);
-  const auto kernel = which == 0 ? paged_tile_kernel<D, false, false> : which == 1 ? paged_tile_kernel<D, false, true>
-                    : which == 2 ? paged_tile_kernel<D, true, false> : paged_tile_kernel<D, true, true>;
-  if (lds > 65536) {
-    static std::atomic<uint64_t> done[4];
-    const int32_t rc = lds_opt_in((const void*)kernel, lds, &done[which]);
-    if (rc != HCA_OK) return rc;
+__global__ __launch_bounds__(256) void paged_tile_join_kernel(PagedView V, AttendArgs a, TilePlan tp, const Partial* __restrict__ ml,
+                                                              const float* __restrict__ part) {
+  constexpr int TPR = D / 4, NG = 256 / TPR;
+  const int h = blockIdx.x % V.hkv;
+  int i;
+  const int b = paged_find(V.n_seqs, blockIdx.x / V.hkv, &i, [&](int s) { int f; return paged_rows(a.cu, s, a.total, &f); });
+  if (b >= V.n_seqs || i >= a.max_q) return;
+  const int L = tile_len(V, a, tp);
+  const TileSeq ts = tile_shares(V, a, tp, L, b);
+  if (ts.ns <= 1) return;
+  const int first = tile_places(V, a, tp, L, b);
+  int row0;
+  (void)paged_rows(a.cu, b, a.total, &row0);
+  const int grp = threadIdx.x / TPR, ch = threadIdx.x % TPR * 4;
+  for (int x = grp; x < V.gqa; x += NG) {               // a group of threads per head
+    const int r = i * V.gqa + x, rt = r / kTileRows;
+    const auto at = [&](int k) { return ((int64_t)(first + rt * ts.ns + k) * V.hkv + h) * kTileRows + r % kTileRows; };
+    float M = -1e30f, sum = 0.f;
+    f4 o = {0.f, 0.f, 0.f, 0.f};
+    for (int k0 = 0; k0 < ts.ns; k0 += 4) {
+      Partial p[4];
+      f4 v[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int64_t z = at(k0 + k < ts.ns ? k0 + k : k0);
+        p[k] = ml[z];
+        v[k] = *reinterpret_cast<const f4*>(part + z * D + ch);
+        if (k0 + k >= ts.ns) p[k] = Partial{-1e30f, 0.f}, v[k] = f4{0.f, 0.f, 0.f, 0.f};
+      }
+      const float next = fmaxf(fmaxf(M, fmaxf(p[0].M, p[1].M)), fmaxf(p[2].M, p[3].M)), f0 = exp2_raw(M - next);
+      sum *= f0;
+      o *= f0;
+      M = next;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float f = exp2_raw(p[k].M - M);
+        sum = fmaf(p[k].l, f, sum);
+        o += v[k] * f;
+      }
+    }
+    const int64_t out = (int64_t)(row0 + i) * V.hq + h * V.gqa + x;
+    if (V.elem == HCA_BF16)
+      write_row<D, true>(V, a, out, ch, o, M, sum);
+    else
+      write_row<D, false>(V, a, out, ch, o, M, sum);
   }
-  kernel<<<(unsigned)(tiles * V.hkv), 256, lds, st>>>(V, a);
-  HCA_HIP(hipGetLastError());
-  return HCA_OK;
 }
 
 // Workgroups per KV head that fill the chip once: two on each of its 256 compute units.
 static int rows_want(const PagedView& V) { return V.hkv >= 512 ? 1 : 512 / V.hkv; }
 constexpr int kOneItem = 256;      // sequences up to this length are one piece, and nothing has to be joined
 
-static int rows_cols(const PagedView& V, int max_q) {
-  const int64_t R = (int64_t)max_q * V.gqa;
-  return R <= 16 ? 16 : R <= 32 ? 32 : 64;
-}
+// Up to 32 query rows per sequence and KV head (queries x heads of the group) go to the rows kernel.
+static bool few_rows(const PagedView& V, int max_q) { return (int64_t)max_q * V.gqa <= 32; }
+static int rows_cols(const PagedView& V, int max_q) { return (int64_t)max_q * V.gqa <= 16 ? 16 : 32; }
 
 template <int D, int NT>
 static int32_t launch_rows_nt(const PagedView& V, const AttendArgs& a, int64_t max_len, void* ws, hipStream_t st) {
@@ -985,11 +1076,38 @@ static int32_t launch_rows_nt(const PagedView& V, const AttendArgs& a, int64_t m
 }
 template <int D>
 static int32_t launch_rows(const PagedView& V, const AttendArgs& a, int64_t max_len, void* ws, hipStream_t st) {
-  switch (rows_cols(V, a.max_q)) {
-    case 16: return launch_rows_nt<D, 1>(V, a, max_len, ws, st);
-    case 32: return launch_rows_nt<D, 2>(V, a, max_len, ws, st);
-    default: return launch_rows_nt<D, 4>(V, a, max_len, ws, st);
+  return rows_cols(V, a.max_q) == 16 ? launch_rows_nt<D, 1>(V, a, max_len, ws, st) : launch_rows_nt<D, 2>(V, a, max_len, ws, st);
+}
+
+// Tiles are divided while they are fewer than what the chip takes at once (two workgroups per compute unit).
+static bool divides_tiles(const PagedView& V, int64_t total_q) { return total_q * V.gqa / kTileRows < rows_want(V); }
+
+template <int D>
+static int32_t launch_tiles(const PagedView& V, const AttendArgs& a, void* ws, hipStream_t st) {
+  constexpr int lds = 2 * 64 * D * 2 * 2 + 2 * 16 * 4;
+  const int64_t tiles = (int64_t)a.total * V.gqa / kTileRows + (a.total < V.n_seqs ? a.total : V.n_seqs);
+  const bool divide = divides_tiles(V, a.total);
+  const TilePlan tp{divide ? rows_want(V) : 0, 2};
+  // a sequence's shares: tiles * ceil(units / L) <= tiles * units / L + tiles
+  const int64_t items = tiles + tp.want;
+  const int64_t rows = 2 * (int64_t)rows_want(V) * V.hkv * kTileRows;
+  Partial* ml = (Partial*)ws;
+  float* part = (float*)((char*)ws + align_up(rows * (int64_t)sizeof(Partial), 256));
+  const int which = (V.elem == HCA_BF16 ? 2 : 0) + (V.code == HCA_E4M3 ? 1 : 0);
+  const auto kernel = which == 0 ? paged_tile_kernel<D, false, false> : which == 1 ? paged_tile_kernel<D, false, true>
+                    : which == 2 ? paged_tile_kernel<D, true, false> : paged_tile_kernel<D, true, true>;
+  if (lds > 65536) {
+    static std::atomic<uint64_t> done[4];
+    const int32_t rc = lds_opt_in((const void*)kernel, lds, &done[which]);
+    if (rc != HCA_OK) return rc;
   }
+  kernel<<<(unsigned)(items * V.hkv), 256, lds, st>>>(V, a, tp, ml, part);
+  HCA_HIP(hipGetLastError());
+  if (divide) {
+    paged_tile_join_kernel<D><<<(unsigned)((int64_t)a.total * V.hkv), 256, 0, st>>>(V, a, tp, ml, part);
+    HCA_HIP(hipGetLastError());
+  }
+  return HCA_OK;
 }
 
 }  // namespace hca
@@ -1002,7 +1120,7 @@ size_t hca_paged_workspace_bytes(const hca_paged_shape* shape, int64_t total_q, 
   PagedView V;
   if (paged_view(shape, &V) != HCA_OK || total_q < 0 || max_q < 0) return 0;
   if (max_q > total_q) max_q = (int32_t)total_q;
-  const int64_t rows = 2 * (int64_t)rows_want(V) * V.hkv * rows_cols(V, max_q);
+  const int64_t rows = 2 * (int64_t)rows_want(V) * V.hkv * (few_rows(V, max_q) ? rows_cols(V, max_q) : kTileRows);
   return (size_t)(align_up(rows * (int64_t)sizeof(Partial), 256) + align_up(rows * V.D * 4, 256) + 256);
 }
 
@@ -1024,9 +1142,9 @@ int32_t hca_paged_attend(const hca_paged_shape* shape, const void* q, int64_t q_
   const AttendArgs a{(const uint16_t*)q, q_stride, cu, lens, tables, (const uint8_t*)kv, scale, (const uint16_t*)open,
                      sm_scale * 1.44269504088896341f, (int32_t)total_q, (int32_t)(max_q < total_q ? max_q : total_q), causal, (uint16_t*)y, lse};
   hipStream_t st = (hipStream_t)stream;
-  if ((int64_t)(max_q < total_q ? max_q : total_q) * V.gqa <= 64)
+  if (few_rows(V, a.max_q))
     return V.D == 128 ? launch_rows<128>(V, a, max_len, workspace, st) : launch_rows<64>(V, a, max_len, workspace, st);
-  return V.D == 128 ? launch_tiles<128>(V, a, st) : launch_tiles<64>(V, a, st);
+  return V.D == 128 ? launch_tiles<128>(V, a, workspace, st) : launch_tiles<64>(V, a, workspace, st);
 }
 
 }  // extern "C"
