@@ -29,8 +29,9 @@ int32_t paged_view(const hca_paged_shape* s, PagedView* V) {
 }
 
 // ---- page tables -----------------------------------------------------------------------------------
-// One workgroup, a thread per sequence: three prefix sums (tokens, pages given back, pages needed) and the pages
-// moved by whole waves.  Nothing but latency: lengths, counts and the free list's top are a few KB.
+// One workgroup, a thread per sequence: prefix sums of the tokens, of the pages given back and of the pages needed, then the pages
+// are moved.  Nothing but latency: lengths, counts and the free list's top are a few KB, so what counts is how many
+// loads and barriers wait for one another.
 struct MapArgs {
   const int32_t *add, *lens_in, *free_in;
   int32_t *lens_out, *tables, *free_pages, *free_out, *start, *cu, *tok_seq, *tok_pos, *tok_slot;
@@ -52,78 +53,107 @@ __device__ __forceinline__ void map_token(const PagedView& V, const MapArgs& a, 
     a.tok_slot[t] = pos < 0 ? -1 : a.tables[(int64_t)lo * V.max_pages + (pos >> V.lp)] * V.P + (pos & (V.P - 1));
 }
 
-constexpr int kMapThreads = 1024;
+// Exclusive prefix sums of N values per thread over a workgroup of NW waves, and their totals: one barrier for all.
+template <int NW, int N>
+__device__ __forceinline__ void map_scan(int64_t (&x)[N], int64_t (&all)[N], uint64_t (*sums)[NW]) {
+  const int w = threadIdx.x >> 6;
+  uint64_t incl[N];
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    incl[k] = wave_scan_incl((uint64_t)x[k]);
+    if ((threadIdx.x & 63) == 63) sums[k][w] = incl[k];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    uint64_t before = 0, total = 0;
+#pragma unroll
+    for (int v = 0; v < NW; ++v) {
+      const uint64_t s = sums[k][v];
+      before += v < w ? s : 0;
+      total += s;
+    }
+    x[k] = (int64_t)(before + incl[k]) - x[k];
+    all[k] = (int64_t)total;
+  }
+}
 
-__global__ __launch_bounds__(kMapThreads) void paged_map_kernel(PagedView V, MapArgs a, int tokens_here) {
-  __shared__ uint64_t wsum[16];
-  __shared__ int32_t s_cu[kPagedMaxSeqs + 1], s_start[kPagedMaxSeqs];
-  __shared__ int32_t s_first[kPagedMaxSeqs], s_count[kPagedMaxSeqs];      // table entries to move
-  __shared__ int64_t s_rank[kPagedMaxSeqs];                               // places in the free list
-  const int b = threadIdx.x, w = b >> 6, lane = b & 63;
+// move(s, j) for every j < count[s] of every sequence s: 64 at a time, the chunks of one sequence dealt out over the waves
+// from wave s on, so that neither a long sequence nor a regular pattern of sequences falls to one wave
+template <int NW, typename F>
+__device__ __forceinline__ void map_pages(int n_seqs, const int32_t* count, F&& move) {
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  for (int s0 = 0; s0 < n_seqs; s0 += 64) {
+    const int c = s0 + lane < n_seqs ? count[s0 + lane] : 0;
+    for (uint64_t some = __ballot(c > 0); some != 0; some &= some - 1) {
+      const int l = __builtin_ctzll(some), cs = __builtin_amdgcn_readlane(c, l), s = s0 + l;
+      for (int j = ((w - __popcll(some)) & (NW - 1)) * 64 + lane; j < cs; j += NW * 64) move(s, j);
+    }
+  }
+}
+
+template <int NW>
+__global__ __launch_bounds__(64 * NW) void paged_map_kernel(PagedView V, MapArgs a, int tokens_here) {
+  constexpr int NS = 64 * NW;
+  __shared__ uint64_t sums[3][NW];
+  __shared__ int64_t s_given[NW];
+  __shared__ int32_t s_cu[NS + 1], s_start[NS], s_first[NS], s_back[NS], s_need[NS];
+  __shared__ int64_t s_back_at[NS], s_need_at[NS];                        // places in the free list
+  const int b = threadIdx.x, w = b >> 6;
   const bool live = b < V.n_seqs;
   const int64_t room = (int64_t)V.max_pages << V.lp;
   int64_t n = live ? a.lens_in[b] : 0;
-  n = n < 0 ? 0 : n > room ? room : n;
   const int add = live ? a.add[b] : 0;
   int64_t fc = a.free_in[0];
+  n = n < 0 ? 0 : n > room ? room : n;
   fc = fc < 0 ? 0 : fc > V.n_pages ? V.n_pages : fc;
   const bool gone = add < 0;
-  const int64_t T = add > 0 ? add : 0;
-  const int64_t held = (n + V.P - 1) >> V.lp;
+  const int64_t T = add > 0 ? add : 0, n0 = gone ? 0 : n;
   // pages of ending sequences go on top of the free list
-  const auto scan = [&](int64_t x, int64_t* all) {
-    uint64_t sum;
-    const int64_t before = (int64_t)block_scan_excl<16>((uint64_t)x, wsum, &sum);
-    *all = (int64_t)sum;
-    return before;
-  };
-  int64_t back_all, need_all, T_all;
-  const int64_t back = gone ? held : 0;
-  const int64_t back_at = scan(back, &back_all);
-  s_first[b] = 0;
-  s_count[b] = (int32_t)back;
-  s_rank[b] = fc + back_at;
-  __syncthreads();
-  for (int s = w; s < V.n_seqs; s += 16) {
-    const int32_t* row = a.tables + (int64_t)s * V.max_pages;
-    for (int j = lane; j < s_count[s]; j += 64)
-      if (s_rank[s] + j < V.n_pages) a.free_pages[s_rank[s] + j] = row[j];
-  }
-  int64_t avail = fc + back_all;
+  int64_t x[2] = {gone ? (n + V.P - 1) >> V.lp : 0, T}, all[2];
+  s_back[b] = (int32_t)x[0];
+  map_scan<NW, 2>(x, all, sums);
+  const int64_t row0 = x[1];
+  s_back_at[b] = fc + x[0];
+  int64_t avail = fc + all[0];
   if (avail > V.n_pages) avail = V.n_pages;
-  const int64_t n0 = gone ? 0 : n;
-  const int64_t row0 = scan(T, &T_all);
   const bool fits = n0 + T <= room && row0 + T <= a.max_new;
   const int64_t first = (n0 + V.P - 1) >> V.lp;
   const int64_t need = fits ? ((n0 + T + V.P - 1) >> V.lp) - first : 0;
-  const int64_t need_at = scan(need, &need_all);
-  const bool ok = fits && (need == 0 || need_at + need <= avail);
-  int64_t given;
-  (void)scan(ok ? need : 0, &given);
+  int64_t y[1] = {need}, total[1];
+  map_scan<NW, 1>(y, total, sums + 2);               // (its barrier also shows every wave the lists above)
+  const bool ok = fits && (need == 0 || y[0] + need <= avail);
   s_first[b] = (int32_t)first;
-  s_count[b] = ok ? (int32_t)need : 0;
-  s_rank[b] = avail - 1 - need_at;
+  s_need[b] = ok ? (int32_t)need : 0;
+  s_need_at[b] = avail - 1 - y[0];
   const int32_t st = ok ? (int32_t)n0 : -1;
   s_start[b] = st;
   s_cu[b] = (int32_t)(row0 < a.max_new ? row0 : a.max_new);
-  if (b == 0) s_cu[V.n_seqs] = (int32_t)(T_all < a.max_new ? T_all : a.max_new);
+  if (b == 0) s_cu[V.n_seqs] = (int32_t)(all[1] < a.max_new ? all[1] : a.max_new);
+  // granted needs are a prefix of the sums: the last one is what was given
+  const uint64_t granted = __ballot(ok && need > 0);
+  if (granted == 0 ? (b & 63) == 0 : (b & 63) == 63 - __builtin_clzll(granted)) s_given[w] = granted == 0 ? 0 : y[0] + need;
+  map_pages<NW>(V.n_seqs, s_back, [&](int s, int j) {
+    if (s_back_at[s] + j < V.n_pages) a.free_pages[s_back_at[s] + j] = a.tables[(int64_t)s * V.max_pages + j];
+  });
   if (live) {
     a.start[b] = st;
     a.lens_out[b] = (int32_t)(n0 + (ok ? T : 0));
     a.cu[b] = s_cu[b];
-    if (b == 0) {
-      a.cu[V.n_seqs] = s_cu[V.n_seqs];
-      a.free_out[0] = (int32_t)(avail - given);
-    }
   }
   __syncthreads();           // the pushed pages are in place, and so are the lists
-  for (int s = w; s < V.n_seqs; s += 16) {
-    int32_t* row = a.tables + (int64_t)s * V.max_pages + s_first[s];
-    for (int j = lane; j < s_count[s]; j += 64) row[j] = a.free_pages[s_rank[s] - j];
+  if (b == 0) {
+    int64_t given = 0;
+    for (int v = 0; v < NW; ++v) given = s_given[v] > given ? s_given[v] : given;
+    a.cu[V.n_seqs] = s_cu[V.n_seqs];
+    a.free_out[0] = (int32_t)(avail - given);
   }
+  map_pages<NW>(V.n_seqs, s_need, [&](int s, int j) {
+    a.tables[(int64_t)s * V.max_pages + s_first[s] + j] = a.free_pages[s_need_at[s] - j];
+  });
   if (!tokens_here) return;
   __syncthreads();
-  for (int t = b; t < s_cu[V.n_seqs]; t += kMapThreads) map_token(V, a, s_cu, s_start, t);
+  for (int t = b; t < s_cu[V.n_seqs]; t += NS) map_token(V, a, s_cu, s_start, t);
 }
 
 // the same for many tokens: a thread each, in a launch of its own
@@ -152,15 +182,37 @@ __device__ __forceinline__ int store_items(const PagedView& V, const StoreArgs& 
   return c > 1 ? c : 1;
 }
 
-// One workgroup per (block, KV head, side).  The block's rows are staged in LDS as they are (rows of D numbers, 8 bytes
-// of padding: the value pieces gather four rows at a time), their largest magnitude is reduced, and every thread codes
-// pieces of 16 numbers in the cache's order.  The workgroup of a sequence's first block also writes the rows that
-// stay open behind the last whole block: it alone reads old open rows, so nothing is overwritten before it is read.
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+// the larger magnitudes of two pairs of numbers: they are ordered like their bits
+__device__ __forceinline__ u16x2 larger(u16x2 m, uint32_t w) {
+  return __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, w & 0x7fff7fffu));
+}
+
+// Four numbers as codes.
+template <bool BF16, bool E4M3>
+__device__ __forceinline__ uint32_t encode(uint32_t w0, uint32_t w1, float inv) {
+  constexpr float kMax = E4M3 ? 448.f : 127.f;
+  float x[4] = {elem_to_float<BF16>(w0 & 0xffffu), elem_to_float<BF16>(w0 >> 16), elem_to_float<BF16>(w1 & 0xffffu), elem_to_float<BF16>(w1 >> 16)};
+#pragma unroll
+  for (int j = 0; j < 4; ++j) x[j] = fminf(fmaxf(x[j] * inv, -kMax), kMax);
+  if (E4M3) return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x[2], x[3], __builtin_amdgcn_cvt_pk_fp8_f32(x[0], x[1], 0, false), true);
+  // rounded to the nearest integer (ties to even) by the addition: the code is the sum's last byte
+  uint32_t u[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) u[j] = __float_as_uint(x[j] + 12582912.f);
+  return __builtin_amdgcn_perm(__builtin_amdgcn_perm(u[3], u[2], 0x0c0c0400u), __builtin_amdgcn_perm(u[1], u[0], 0x0c0c0400u), 0x05040100u);
+}
+
+// One workgroup per (block, KV head, side); a thread codes up to four pieces of 16 numbers in the cache's order.  Keys: a piece is 32
+// bytes of one row, straight from memory.  Values: a piece has four channels of four rows, so the rows go through LDS (16
+// bytes of padding per row: the four rows that a wave gathers at once lie in different banks).  The workgroup of a
+// sequence's first block also writes the rows that stay open behind the last whole block: it alone reads old open rows, so
+// nothing is overwritten before it is read.
 template <int D, bool BF16, bool E4M3>
 __global__ __launch_bounds__(256) void paged_store_kernel(PagedView V, StoreArgs a) {
-  constexpr int RS = D + 4;                     // row stride in LDS
+  constexpr int RS = D + 8, PT = D / 16 * 16;   // row stride in LDS, pieces per tile of 16 tokens
   extern __shared__ uint16_t rows[];            // [P][RS]
-  __shared__ float wmax[4];
+  __shared__ uint32_t wmax[4];
   const int h = blockIdx.y, side = blockIdx.z, tid = threadIdx.x;
   int m;
   const int b = paged_find(V.n_seqs, blockIdx.x, &m, [&](int s) { return store_items(V, a, s); });
@@ -175,70 +227,96 @@ __global__ __launch_bounds__(256) void paged_store_kernel(PagedView V, StoreArgs
   const int64_t stride = a.stride[side];
   uint16_t* open = a.open + (((int64_t)b * V.hkv + h) * 2 + side) * V.side();
   if (whole > 0) {
+    const int page = nb < V.max_pages ? a.tables[(int64_t)b * V.max_pages + nb] : -1;
     const int64_t p0 = (int64_t)nb << V.lp;
     const int old = p0 < start ? (int)(start - p0) : 0;      // rows that are in the open rows
-    for (int i = tid; i < P * (D / 4); i += 256) {           // 8 bytes at a time
-      const int o = i / (D / 4), ch = i % (D / 4) * 4;
-      uint2 v;
-      if (o >= old) {
-        v = *reinterpret_cast<const uint2*>(src + (row0 + (p0 + o - start)) * stride + ch);
-      } else {
-        uint32_t e[4];
+    const int pieces = P * (D / 16);
+    const uint16_t* from = src + (row0 + (p0 - start)) * stride;
+    uint4 x[4][2];
+    u16x2 top = {0, 0};
+    if (side == 0) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) e[k] = open[side == 0 ? key_at(o, ch + k, D) : value_at(o, ch + k, D)];
-        v = uint2{e[0] | e[1] << 16, e[2] | e[3] << 16};
+      for (int k = 0; k < 4; ++k) {
+        const int i = tid + 256 * k, r = i % PT, t = i / PT * 16 + (r & 15), ch = 16 * (r >> 4);
+        x[k][0] = x[k][1] = uint4{0, 0, 0, 0};
+        if (i < pieces) {
+          const uint4* p = reinterpret_cast<const uint4*>(t >= old ? from + t * stride + ch : open + (int64_t)i * 16);
+          x[k][0] = p[0];
+          x[k][1] = p[1];
+        }
       }
-      *reinterpret_cast<uint2*>(rows + o * RS + ch) = v;
+    } else {
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int z = 0; z < 2; ++z) {
+          const int i = tid + 256 * (2 * k + z), t = i / (D / 8), ch = i % (D / 8) * 8;
+          x[k][z] = t >= old && t < P ? *reinterpret_cast<const uint4*>(from + t * stride + ch) : uint4{0, 0, 0, 0};
+        }
     }
-    __syncthreads();
-    float amax = 0.f;
-    for (int i = tid; i < P * (D / 4); i += 256) {
-      const uint2 v = *reinterpret_cast<const uint2*>(rows + i / (D / 4) * RS + i % (D / 4) * 4);
-      amax = fmaxf(amax, fmaxf(fmaxf(fabsf(elem_to_float<BF16>(v.x & 0xffffu)), fabsf(elem_to_float<BF16>(v.x >> 16))),
-                               fmaxf(fabsf(elem_to_float<BF16>(v.y & 0xffffu)), fabsf(elem_to_float<BF16>(v.y >> 16)))));
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+      for (int z = 0; z < 2; ++z) {
+        top = larger(larger(larger(larger(top, x[k][z].x), x[k][z].y), x[k][z].z), x[k][z].w);
+        if (side == 1) {
+          const int i = tid + 256 * (2 * k + z), t = i / (D / 8), ch = i % (D / 8) * 8;
+          if (t >= old && t < P) *reinterpret_cast<uint4*>(rows + t * RS + ch) = x[k][z];
+        }
+      }
+    if (side == 1 && old > 0) {                              // old rows, in the cache's order
+      for (int i = tid; i < (old + 15) / 16 * PT; i += 256) {
+        const int r = i % PT, t = i / PT * 16 + 4 * ((r >> 4) & 3), ch = 64 * (r >> 6) + (r & 15);
+        const uint2* p = reinterpret_cast<const uint2*>(open + (int64_t)i * 16);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const uint2 v = p[u];
+          const uint32_t e[4] = {v.x & 0xffffu, v.x >> 16, v.y & 0xffffu, v.y >> 16};
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            if (t + j < old) {
+              rows[(t + j) * RS + ch + 16 * u] = (uint16_t)e[j];
+              top = larger(top, e[j]);
+            }
+        }
+      }
     }
-    amax = wave_max(amax);
-    if ((tid & 63) == 0) wmax[tid >> 6] = amax;
+    const uint32_t mx = wave_max((uint32_t)(top.x > top.y ? top.x : top.y));
+    if ((tid & 63) == 0) wmax[tid >> 6] = mx;
     __syncthreads();
-    amax = fmaxf(fmaxf(wmax[0], wmax[1]), fmaxf(wmax[2], wmax[3]));
-    constexpr float kMax = E4M3 ? 448.f : 127.f;
-    float scale = amax / kMax;
+    uint32_t bits = wmax[0];
+#pragma unroll
+    for (int k = 1; k < 4; ++k) bits = wmax[k] > bits ? wmax[k] : bits;
+    float scale = elem_to_float<BF16>(bits) / (E4M3 ? 448.f : 127.f);
     if (!(scale >= 0x1p-64f)) scale = 0x1p-64f;
     const float inv = 1.0f / scale;
-    const int page = nb < V.max_pages ? a.tables[(int64_t)b * V.max_pages + nb] : -1;
     if (page >= 0 && page < V.n_pages) {
-      uint8_t* out = a.kv + (((int64_t)page * V.hkv + h) * 2 + side) * V.side();
+      uint4* out = reinterpret_cast<uint4*>(a.kv + (((int64_t)page * V.hkv + h) * 2 + side) * V.side());
       if (tid == 0) a.scale[((int64_t)page * V.hkv + h) * 2 + side] = scale;
-      for (int i = tid; i < P * D / 16; i += 256) {            // piece i: 16 codes
-        const int tile = i / (D / 16 * 16), r = i % (D / 16 * 16), hh = r >> 6, g = (r >> 4) & 3, l = r & 15;
-        uint32_t wd[4];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          float x[4];
+      for (int k = 0; k < 4; ++k) {
+        const int i = tid + 256 * k;
+        if (i >= pieces) break;
+        uint32_t wd[8];
+        if (side == 0) {
+          const uint32_t e[8] = {x[k][0].x, x[k][0].y, x[k][0].z, x[k][0].w, x[k][1].x, x[k][1].y, x[k][1].z, x[k][1].w};
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            // keys: token l, channel 64 hh + 16 g + 4 k + j; values: token 4 g + j, channel 64 hh + 16 k + l
-            const int t = 16 * tile + (side == 0 ? l : 4 * g + j);
-            const int ch = 64 * hh + (side == 0 ? 16 * g + 4 * k + j : 16 * k + l);
-            const float y = elem_to_float<BF16>(rows[t * RS + ch]) * inv;
-            x[j] = fminf(fmaxf(y, -kMax), kMax);
-          }
-          if (E4M3) {
-            int p = __builtin_amdgcn_cvt_pk_fp8_f32(x[0], x[1], 0, false);
-            p = __builtin_amdgcn_cvt_pk_fp8_f32(x[2], x[3], p, true);
-            wd[k] = (uint32_t)p;
-          } else {
-            wd[k] = 0;
+          for (int z = 0; z < 8; ++z) wd[z] = e[z];
+        } else {
+          const int r = i % PT, t = i / PT * 16 + 4 * ((r >> 4) & 3), ch = 64 * (r >> 6) + (r & 15);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) wd[k] |= ((uint32_t)(int)rintf(x[j]) & 255u) << (8 * j);
+          for (int z = 0; z < 8; ++z) {                      // number 2 z: row 2 (z & 1), channel 16 (z / 2)
+            const uint16_t* p = rows + (t + 2 * (z & 1)) * RS + ch + 16 * (z >> 1);
+            wd[z] = p[0] | (uint32_t)p[RS] << 16;
           }
         }
-        reinterpret_cast<uint4*>(out)[i] = uint4{wd[0], wd[1], wd[2], wd[3]};
+        out[i] = uint4{encode<BF16, E4M3>(wd[0], wd[1], inv), encode<BF16, E4M3>(wd[2], wd[3], inv),
+                       encode<BF16, E4M3>(wd[4], wd[5], inv), encode<BF16, E4M3>(wd[6], wd[7], inv)};
       }
     }
   }
   if (m != 0) return;
-  // rows of the block that stays open (all new ones, if no block became whole)
+  // rows of the block that stays open (all new ones, if no block became whole); old ones have been read: see the barrier
   const int64_t first = whole > 0 ? end >> V.lp << V.lp : start;
   const int left = (int)(end - first);
   for (int i = tid; i < left * D; i += 256) {
@@ -250,7 +328,7 @@ __global__ __launch_bounds__(256) void paged_store_kernel(PagedView V, StoreArgs
 
 template <int D, bool BF16>
 static int32_t launch_store(const PagedView& V, const StoreArgs& a, dim3 grid, hipStream_t st) {
-  const int lds = V.P * (D + 4) * 2;
+  const int lds = V.P * (D + 8) * 2;
   if (V.code == HCA_E4M3)
     paged_store_kernel<D, BF16, true><<<grid, 256, lds, st>>>(V, a);
   else
@@ -293,7 +371,10 @@ int32_t hca_paged_map(const hca_paged_shape* shape, const int32_t* add, const in
   const MapArgs a{add, lens_in, free_in, lens_out, tables, free_pages, free_out, start, cu, tok_seq, tok_pos, tok_slot, max_new};
   const bool tokens = (tok_seq != nullptr || tok_pos != nullptr || tok_slot != nullptr) && max_new > 0;
   const bool here = tokens && max_new <= 2048;
-  paged_map_kernel<<<1, kMapThreads, 0, (hipStream_t)stream>>>(V, a, here ? 1 : 0);
+  if (V.n_seqs <= 256)
+    paged_map_kernel<4><<<1, 256, 0, (hipStream_t)stream>>>(V, a, here ? 1 : 0);
+  else
+    paged_map_kernel<16><<<1, 1024, 0, (hipStream_t)stream>>>(V, a, here ? 1 : 0);
   HCA_HIP(hipGetLastError());
   if (tokens && !here) {
     paged_slots_kernel<<<(unsigned)((max_new + 255) / 256), 256, 0, (hipStream_t)stream>>>(V, a);

@@ -232,12 +232,12 @@ struct Partial {          // of one item, KV head and row: reference, sum; the w
   float M, l;
 };
 
-template <int D, int NT, bool BF16, bool E4M3>
-__global__ __launch_bounds__(256, 2) void paged_rows_kernel(PagedView V, AttendArgs a, SplitPlan sp,
+template <int D, int NT, int NW, bool BF16, bool E4M3>
+__global__ __launch_bounds__(64 * NW, 2) void paged_rows_kernel(PagedView V, AttendArgs a, SplitPlan sp,
                                                                           Partial* __restrict__ ml, float* __restrict__ part) {
   constexpr int NH = D / 64, NC = D / 16, COLS = 16 * NT;
   constexpr int TT = NT == 1 ? 4 : 2, STEP = 16 * TT;  // tiles and tokens that a wave works on at a time
-  extern __shared__ float lds[];                       // [4][COLS][D + 4], then M and l of each wave [4][COLS]
+  extern __shared__ float lds[];                       // [NW][COLS][D + 4], then M and l of each wave [NW][COLS]
   const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int h = blockIdx.y, G = V.gqa;
@@ -284,10 +284,10 @@ __global__ __launch_bounds__(256, 2) void paged_rows_kernel(PagedView V, AttendA
     const int n = sq.n, whole = n >> V.lp << V.lp;
     const int R = m * G;                               // rows in use
 
-    // whole pages: steps of STEP tokens, wave w takes every fourth
+    // whole pages: steps of STEP tokens, wave w takes every NW-th
     const int t_begin = u * kUnit, t_end = ue * kUnit < whole ? ue * kUnit : whole;
     const int steps = t_end > t_begin ? (t_end - t_begin + STEP - 1) / STEP : 0;
-    const int nk = steps > w ? (steps - w + 3) / 4 : 0;
+    const int nk = steps > w ? (steps - w + NW - 1) / NW : 0;
     constexpr int LS = TT == 4 ? 6 : 5;
     const int lpe = V.lp < LS ? V.lp : LS;              // pages smaller than a step: STEP >> lpe of them
     const int per = STEP >> lpe, group = 64 / per;      // pages per step, steps whose pages the lanes hold
@@ -295,7 +295,7 @@ __global__ __launch_bounds__(256, 2) void paged_rows_kernel(PagedView V, AttendA
     // lane j holds page j % per of the wave's step k0 + j / per: its number (-1: no tokens) and scales.  The next group's
     // numbers are asked for when a group begins, its scales one step later.
     const auto ask_id = [&](int k0) {
-      const int k = k0 + lane / per, t = t_begin + (w + 4 * k) * STEP + (lane % per << lpe);
+      const int k = k0 + lane / per, t = t_begin + (w + NW * k) * STEP + (lane % per << lpe);
       return k < nk && t < t_end ? table[t >> V.lp] : -1;
     };
     const auto ask_scale = [&](int id) {
@@ -408,7 +408,7 @@ __global__ __launch_bounds__(256, 2) void paged_rows_kernel(PagedView V, AttendA
 #pragma unroll
       for (int tt = 0; tt < TT; ++tt) {
         const int pg = __builtin_amdgcn_readlane(id, (k % group) * per + (16 * tt >> lpe));
-        const int t = t_begin + (w + 4 * k) * STEP + 16 * tt;
+        const int t = t_begin + (w + NW * k) * STEP + 16 * tt;
         const uint8_t* p = a.kv + ((int64_t)pg * V.hkv + h) * 2 * side + (t & (V.P - 1)) * D + off;
         const bool there = pg >= 0 && pg < V.n_pages;
 #pragma unroll
@@ -425,7 +425,7 @@ __global__ __launch_bounds__(256, 2) void paged_rows_kernel(PagedView V, AttendA
     // open rows, a tile at a time, where the piece ends the sequence: the same with halves made from the rows themselves, while
     // the first codes are on their way; by the waves that have the fewest steps
     if (ue == units) {
-      for (int t0 = whole + 16 * (3 - w); t0 < n; t0 += 64) {
+      for (int t0 = whole + 16 * (NW - 1 - w); t0 < n; t0 += 16 * NW) {
         const uint16_t* kp = a.open + ((int64_t)b * V.hkv + h) * 2 * side + (t0 & (V.P - 1)) * D;
         uint4 raw[2][NH][2];
 #pragma unroll
@@ -501,7 +501,7 @@ __global__ __launch_bounds__(256, 2) void paged_rows_kernel(PagedView V, AttendA
         load(k + 1, kw, 0);
       }
       h2 p[NT][TT][2];
-      weigh(std::integral_constant<int, TT>{}, s, ks, lv, iv, t_begin + (w + 4 * k) * STEP, t_end, p);
+      weigh(std::integral_constant<int, TT>{}, s, ks, lv, iv, t_begin + (w + NW * k) * STEP, t_end, p);
 #pragma unroll
       for (int pr = 0; pr < TT / 2; ++pr) {
         h8 pb[NT];
@@ -519,10 +519,10 @@ __global__ __launch_bounds__(256, 2) void paged_rows_kernel(PagedView V, AttendA
       if (more) load(k + 1, vw, side);
     }
 
-    // the four waves' results are joined
+    // the waves' results are joined
     constexpr int RS = D + 4;
-    float* sM = lds + 4 * COLS * RS;
-    float* sl = sM + 4 * COLS;
+    float* sM = lds + NW * COLS * RS;
+    float* sl = sM + NW * COLS;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       const float sum = rows_sum(l[nt]);
@@ -537,13 +537,15 @@ __global__ __launch_bounds__(256, 2) void paged_rows_kernel(PagedView V, AttendA
     __syncthreads();
     const bool only = u == 0 && ue == units;
     constexpr int TPR = D / 4;                          // threads per row, four channels each
-    for (int r = threadIdx.x / TPR; r < R; r += 256 / TPR) {
+    for (int r = threadIdx.x / TPR; r < R; r += 64 * NW / TPR) {
       const int ch = threadIdx.x % TPR * 4;
-      const float top = fmaxf(fmaxf(sM[r], sM[COLS + r]), fmaxf(sM[2 * COLS + r], sM[3 * COLS + r]));
+      float top = sM[r];
+#pragma unroll
+      for (int x = 1; x < NW; ++x) top = fmaxf(top, sM[x * COLS + r]);
       float sum = 0.f;
       f4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int x = 0; x < 4; ++x) {
+      for (int x = 0; x < NW; ++x) {
         const float f = exp2_raw(sM[x * COLS + r] - top);
         sum = fmaf(sl[x * COLS + r], f, sum);
         o += *reinterpret_cast<const f4*>(lds + (x * COLS + r) * RS + ch) * f;
@@ -991,24 +993,23 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedView V, AttendA
   if (hh == 0 && a.lse != nullptr) a.lse[at] = l > 0.f ? (M + log2f(l)) * 0.693147180559945309f : -INFINITY;
 }
 
-// Joins the shares of the tiles of divided sequences.  One workgroup per query and KV head.
+// Joins the shares of the tiles of divided sequences: a group of D / 4 threads per query row and head.
 template <int D>
 __global__ __launch_bounds__(256) void paged_tile_join_kernel(PagedView V, AttendArgs a, TilePlan tp, const Partial* __restrict__ ml,
                                                               const float* __restrict__ part) {
   constexpr int TPR = D / 4, NG = 256 / TPR;
   const int h = blockIdx.x % V.hkv;
   int i;
-  const int b = paged_find(V.n_seqs, blockIdx.x / V.hkv, &i, [&](int s) { int f; return paged_rows(a.cu, s, a.total, &f); });
-  if (b >= V.n_seqs || i >= a.max_q) return;
+  const int b = paged_find(V.n_seqs, blockIdx.x / V.hkv, &i, [&](int s) { return (seq_rows(V, a, s) + NG - 1) / NG; });
+  if (b >= V.n_seqs) return;
   const int L = tile_len(V, a, tp);
   const TileSeq ts = tile_shares(V, a, tp, L, b);
   if (ts.ns <= 1) return;
   const int first = tile_places(V, a, tp, L, b);
   int row0;
   (void)paged_rows(a.cu, b, a.total, &row0);
-  const int grp = threadIdx.x / TPR, ch = threadIdx.x % TPR * 4;
-  for (int x = grp; x < V.gqa; x += NG) {               // a group of threads per head
-    const int r = i * V.gqa + x, rt = r / kTileRows;
+  const int r = i * NG + threadIdx.x / TPR, rt = r / kTileRows, ch = threadIdx.x % TPR * 4;
+  if (r < seq_rows(V, a, b)) {
     const auto at = [&](int k) { return ((int64_t)(first + rt * ts.ns + k) * V.hkv + h) * kTileRows + r % kTileRows; };
     float M = -1e30f, sum = 0.f;
     f4 o = {0.f, 0.f, 0.f, 0.f};
@@ -1033,7 +1034,7 @@ __global__ __launch_bounds__(256) void paged_tile_join_kernel(PagedView V, Atten
         o += v[k] * f;
       }
     }
-    const int64_t out = (int64_t)(row0 + i) * V.hq + h * V.gqa + x;
+    const int64_t out = (int64_t)(row0 + r / V.gqa) * V.hq + h * V.gqa + r % V.gqa;
     if (V.elem == HCA_BF16)
       write_row<D, true>(V, a, out, ch, o, M, sum);
     else
@@ -1043,32 +1044,30 @@ __global__ __launch_bounds__(256) void paged_tile_join_kernel(PagedView V, Atten
 
 // Workgroups per KV head that fill the chip once: two on each of its 256 compute units.
 static int rows_want(const PagedView& V) { return V.hkv >= 512 ? 1 : 512 / V.hkv; }
-constexpr int kOneItem = 256;      // sequences up to this length are one piece, and nothing has to be joined
+constexpr int kOneItem = 1024;     // sequences up to this length are one piece, and nothing has to be joined
 
 // Up to 32 query rows per sequence and KV head (queries x heads of the group) go to the rows kernel.
 static bool few_rows(const PagedView& V, int max_q) { return (int64_t)max_q * V.gqa <= 32; }
 static int rows_cols(const PagedView& V, int max_q) { return (int64_t)max_q * V.gqa <= 16 ? 16 : 32; }
 
-template <int D, int NT>
-static int32_t launch_rows_nt(const PagedView& V, const AttendArgs& a, int64_t max_len, void* ws, hipStream_t st) {
-  constexpr int lds = 4 * 16 * NT * (D + 4 + 2) * 4;
-  const bool one = max_len <= kOneItem;
-  const SplitPlan sp{one ? 0 : rows_want(V), 4};
+template <int D, int NT, int NW>
+static int32_t launch_rows_nt(const PagedView& V, const AttendArgs& a, const SplitPlan& sp, void* ws, hipStream_t st) {
+  constexpr int lds = NW * 16 * NT * (D + 4 + 2) * 4;
   const int64_t rows = 2 * (int64_t)rows_want(V) * V.hkv * 16 * NT;
   Partial* ml = (Partial*)ws;
   float* part = (float*)((char*)ws + align_up(rows * (int64_t)sizeof(Partial), 256));
-  const dim3 grid((unsigned)(one ? (a.total < V.n_seqs ? a.total : V.n_seqs) : sp.want), (unsigned)V.hkv);
+  const dim3 grid((unsigned)(sp.want == 0 ? (a.total < V.n_seqs ? a.total : V.n_seqs) : sp.want), (unsigned)V.hkv);
   const int which = (V.elem == HCA_BF16 ? 2 : 0) + (V.code == HCA_E4M3 ? 1 : 0);
-  const auto kernel = which == 0 ? paged_rows_kernel<D, NT, false, false> : which == 1 ? paged_rows_kernel<D, NT, false, true>
-                    : which == 2 ? paged_rows_kernel<D, NT, true, false> : paged_rows_kernel<D, NT, true, true>;
+  const auto kernel = which == 0 ? paged_rows_kernel<D, NT, NW, false, false> : which == 1 ? paged_rows_kernel<D, NT, NW, false, true>
+                    : which == 2 ? paged_rows_kernel<D, NT, NW, true, false> : paged_rows_kernel<D, NT, NW, true, true>;
   if (lds > 65536) {
     static std::atomic<uint64_t> done[4];
     const int32_t rc = lds_opt_in((const void*)kernel, lds, &done[which]);
     if (rc != HCA_OK) return rc;
   }
-  kernel<<<grid, 256, lds, st>>>(V, a, sp, ml, part);
+  kernel<<<grid, 64 * NW, lds, st>>>(V, a, sp, ml, part);
   HCA_HIP(hipGetLastError());
-  if (!one) {
+  if (sp.want != 0) {
     paged_join_kernel<D><<<dim3((unsigned)a.total, (unsigned)V.hq), 256, 0, st>>>(V, a, sp, 16 * NT, ml, part);
     HCA_HIP(hipGetLastError());
   }
@@ -1076,7 +1075,11 @@ static int32_t launch_rows_nt(const PagedView& V, const AttendArgs& a, int64_t m
 }
 template <int D>
 static int32_t launch_rows(const PagedView& V, const AttendArgs& a, int64_t max_len, void* ws, hipStream_t st) {
-  return rows_cols(V, a.max_q) == 16 ? launch_rows_nt<D, 1>(V, a, max_len, ws, st) : launch_rows_nt<D, 2>(V, a, max_len, ws, st);
+  const SplitPlan sp{max_len <= kOneItem ? 0 : rows_want(V), 4};
+  // sequences in one piece that leave compute units idle: eight waves instead of four share a piece
+  const bool wide = sp.want == 0 && (int64_t)(a.total < V.n_seqs ? a.total : V.n_seqs) * V.hkv <= 256;
+  if (rows_cols(V, a.max_q) == 16) return wide ? launch_rows_nt<D, 1, 8>(V, a, sp, ws, st) : launch_rows_nt<D, 1, 4>(V, a, sp, ws, st);
+  return wide ? launch_rows_nt<D, 2, 8>(V, a, sp, ws, st) : launch_rows_nt<D, 2, 4>(V, a, sp, ws, st);
 }
 
 // Tiles are divided while they are fewer than what the chip takes at once (two workgroups per compute unit).
@@ -1104,7 +1107,8 @@ static int32_t launch_tiles(const PagedView& V, const AttendArgs& a, void* ws, h
   kernel<<<(unsigned)(items * V.hkv), 256, lds, st>>>(V, a, tp, ml, part);
   HCA_HIP(hipGetLastError());
   if (divide) {
-    paged_tile_join_kernel<D><<<(unsigned)((int64_t)a.total * V.hkv), 256, 0, st>>>(V, a, tp, ml, part);
+    const int64_t groups = (int64_t)a.total * V.gqa / (1024 / D) + (a.total < V.n_seqs ? a.total : V.n_seqs);
+    paged_tile_join_kernel<D><<<(unsigned)(groups * V.hkv), 256, 0, st>>>(V, a, tp, ml, part);
     HCA_HIP(hipGetLastError());
   }
   return HCA_OK;
