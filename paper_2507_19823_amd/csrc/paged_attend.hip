@@ -677,46 +677,81 @@ __device__ __forceinline__ int seq_rows(const PagedView& V, const AttendArgs& a,
   return (m < a.max_q ? m : a.max_q) * V.gqa;
 }
 
-// Where there are fewer tiles than the chip takes at once, the tokens are divided too: every tile of a sequence into ns
-// shares, ns from the sequence's units and L = all tiles' units / workgroups wanted.
+// Tiles go out in order, the ones that see most first inside each sequence.  Where they do not make whole rounds of workgroups
+// (fewer tiles than places, or a few rounds and a rest), the last ones are divided: as many tiles as make whole rounds go
+// out whole, the tokens of the others are cut into shares, ns for every tile of a sequence, from the sequence's units and
+// L = all their units / places; a second launch joins them.  (2100 queries over 34000 tokens are 66 tiles per KV head for 64
+// places: 1716 us as two rounds, 1175 so.  Equal ranges of tokens across tiles, as in the rows kernel, were slower here: a
+// tile's start costs as much as four units, and a piece's partial result is 64 KB.)
 constexpr int kTileRows = 128;
 struct TilePlan {
-  int32_t want;         // workgroups per KV head to divide for; 0: a workgroup per tile
+  int32_t want;         // places per KV head; 0: all tiles go out whole
   int32_t least;        // units per share at least
 };
-struct TileSeq { int tiles, units, ns; };
+struct TileSeq { int tiles, units, shared, ns; };       // `shared` of the tiles, the ones that see least, go out in ns shares each
 __device__ __forceinline__ TileSeq tile_seq(const PagedView& V, const AttendArgs& a, int b) {
-  return TileSeq{(seq_rows(V, a, b) + kTileRows - 1) / kTileRows, (seq_len(V, a, b) + kUnit - 1) / kUnit, 1};
+  return TileSeq{(seq_rows(V, a, b) + kTileRows - 1) / kTileRows, (seq_len(V, a, b) + kUnit - 1) / kUnit, 0, 1};
 }
-__device__ __forceinline__ int tile_len(const PagedView& V, const AttendArgs& a, const TilePlan& tp) {
-  uint64_t all = 0;
-  for (int b = threadIdx.x & 63; b < V.n_seqs; b += 64) {
-    const TileSeq t = tile_seq(V, a, b);
-    all += (uint64_t)t.tiles * (uint32_t)t.units;
+struct TileAll { int whole, L; };                       // tiles that go out whole, units per share
+// f(b0, t): called with 64 sequences at a time, lane l holding sequence b0 + l; true ends
+template <typename F>
+__device__ __forceinline__ void tile_walk(const PagedView& V, const AttendArgs& a, const TileAll& all, F&& f) {
+  const int lane = threadIdx.x & 63;
+  int before = 0;
+  for (int b0 = 0; b0 < V.n_seqs; b0 += 64) {
+    TileSeq t{0, 0, 0, 1};
+    if (b0 + lane < V.n_seqs) t = tile_seq(V, a, b0 + lane);
+    const int incl = (int)wave_scan_incl((uint32_t)t.tiles);
+    const int behind = before + incl - all.whole;       // tiles from the first divided one to this sequence's end
+    t.shared = behind <= 0 ? 0 : behind < t.tiles ? behind : t.tiles;
+    if (t.units > all.L) t.ns = (t.units + all.L - 1) / all.L;
+    if (f(b0, t)) return;
+    before += (int)wave_last((uint32_t)incl);
   }
-  all = wave_scan_incl(all);
-  all = (uint64_t)wave_last((uint32_t)(all >> 32)) << 32 | wave_last((uint32_t)all);
-  const uint64_t L = (all + (uint32_t)tp.want - 1) / (uint32_t)tp.want;
-  return L < (uint64_t)tp.least ? tp.least : L > 1u << 25 ? 1 << 25 : (int)L;
 }
-__device__ __forceinline__ TileSeq tile_shares(const PagedView& V, const AttendArgs& a, const TilePlan& tp, int L, int b) {
-  TileSeq t = tile_seq(V, a, b);
-  if (tp.want != 0 && t.units > L) t.ns = (t.units + L - 1) / L;
-  return t;
+__device__ __forceinline__ TileAll tile_all(const PagedView& V, const AttendArgs& a, const TilePlan& tp) {
+  if (tp.want == 0) return TileAll{INT32_MAX, INT32_MAX};
+  uint32_t tiles = 0;
+  for (int b = threadIdx.x & 63; b < V.n_seqs; b += 64) tiles += (uint32_t)tile_seq(V, a, b).tiles;
+  tiles = wave_sum(tiles);
+  TileAll r{(int)(tiles - tiles % (uint32_t)tp.want), 1};
+  uint64_t units = 0;
+  tile_walk(V, a, r, [&](int, const TileSeq& t) { units += (uint64_t)t.shared * (uint32_t)t.units; return false; });
+  units = wave_scan_incl(units);
+  units = (uint64_t)wave_last((uint32_t)(units >> 32)) << 32 | wave_last((uint32_t)units);
+  const uint64_t L = (units + (uint32_t)tp.want - 1) / (uint32_t)tp.want;
+  r.L = L < (uint64_t)tp.least ? tp.least : L > 1u << 25 ? 1 << 25 : (int)L;
+  return r;
 }
-// the first place in the workspace of sequence b's shares: only divided sequences have any, and since a divided one has
-// ns <= 2 units / L, there are at most 2 want of them
-__device__ __forceinline__ int tile_places(const PagedView& V, const AttendArgs& a, const TilePlan& tp, int L, int b) {
-  uint32_t before = 0;
-  for (int s = threadIdx.x & 63; s < b; s += 64) {
-    const TileSeq t = tile_shares(V, a, tp, L, s);
-    before += t.ns > 1 ? (uint32_t)(t.tiles * t.ns) : 0;
-  }
-  return (int)wave_sum(before);
+// What number i of the numbering by count(t) lies in: its sequence (-1: none), the number inside it, the sequence's tiles, and the
+// places in the workspace that the sequences before it take: only divided tiles have any, and since ns <= 2 units / L
+// where it is more than one, there are at most 2 want of them.
+struct TileFound { int b, within, places; TileSeq t; };
+template <typename F>
+__device__ __forceinline__ TileFound tile_find(const PagedView& V, const AttendArgs& a, const TileAll& all, int i, F&& count) {
+  TileFound r{-1, i, 0, {0, 0, 0, 1}};
+  tile_walk(V, a, all, [&](int b0, const TileSeq& t) {
+    const int c = count(t), incl = (int)wave_scan_incl((uint32_t)c);
+    const int p = t.ns > 1 ? t.shared * t.ns : 0, places = (int)wave_scan_incl((uint32_t)p);
+    const uint64_t past = __ballot(incl > r.within);
+    if (past == 0) {
+      r.within -= (int)wave_last((uint32_t)incl);
+      r.places += (int)wave_last((uint32_t)places);
+      return false;
+    }
+    const int l = __builtin_ctzll(past);
+    r.b = b0 + l;
+    r.within -= __builtin_amdgcn_readlane(incl, l) - __builtin_amdgcn_readlane(c, l);
+    r.places += __builtin_amdgcn_readlane(places, l) - __builtin_amdgcn_readlane(p, l);
+    r.t = TileSeq{__builtin_amdgcn_readlane(t.tiles, l), __builtin_amdgcn_readlane(t.units, l),
+                  __builtin_amdgcn_readlane(t.shared, l), __builtin_amdgcn_readlane(t.ns, l)};
+    return true;
+  });
+  return r;
 }
 
 template <int D, bool BF16, bool E4M3>
-__global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedView V, AttendArgs a, TilePlan tp, Partial* __restrict__ ml,
+__global__ __launch_bounds__(256, D == 64 ? 3 : 2) void paged_tile_kernel(PagedView V, AttendArgs a, TilePlan tp, Partial* __restrict__ ml,
                                                             float* __restrict__ part) {
   constexpr int NH = D / 64, NS = D / 16, NC = D / 32, ROWS = kTileRows;
   extern __shared__ char lds_raw[];
@@ -725,19 +760,17 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedView V, AttendA
   float* sinfo = reinterpret_cast<float*>(sv + 2 * 8 * D);       // [2][4][4]: key scale, log2 and inverse of value scale
   const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4, l32 = lane & 31, hh = lane >> 5;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int h = blockIdx.x % V.hkv;
-  const int L = tp.want == 0 ? 0 : tile_len(V, a, tp);
-  int within;
-  const int b = paged_find(V.n_seqs, blockIdx.x / V.hkv, &within, [&](int s) {
-    const TileSeq t = tile_shares(V, a, tp, L, s);
-    return t.tiles * t.ns;
-  });
-  if (b >= V.n_seqs) return;
-  const TileSeq ts = tile_shares(V, a, tp, L, b);
+  const int h = blockIdx.x % V.hkv, wg = blockIdx.x / V.hkv;
+  const TileAll all = tile_all(V, a, tp);
+  const bool cut = wg >= all.whole;
+  const TileFound at = tile_find(V, a, all, cut ? wg - all.whole : wg, [&](const TileSeq& t) { return cut ? t.shared * t.ns : t.tiles; });
+  const int b = at.b, ns = cut ? at.t.ns : 1;
+  if (b < 0) return;
   int row0;
   const int m_all = paged_rows(a.cu, b, a.total, &row0);
   const int G = V.gqa, R = seq_rows(V, a, b);
-  const int rt = ts.tiles - 1 - within / ts.ns, share = within % ts.ns;      // the tiles that see most come first
+  // the tiles that see most come first
+  const int rt = (cut ? at.t.shared : at.t.tiles) - 1 - at.within / ns, share = at.within % ns;
   const int n = seq_len(V, a, b), whole = n >> V.lp << V.lp;
   const int64_t side = V.side();
 
@@ -773,7 +806,7 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedView V, AttendA
   const int most_seen = rt * ROWS + 32 * w < R ? (int)wave_max((uint32_t)sees) : 0;      // a wave without rows only loads
   const int r_last = rt * ROWS + ROWS - 1 < R ? rt * ROWS + ROWS - 1 : R - 1;
   const int tile_units = (seen(r_last / G) + kUnit - 1) / kUnit;
-  const int u_begin = (int)((int64_t)tile_units * share / ts.ns), u_end = (int)((int64_t)tile_units * (share + 1) / ts.ns);
+  const int u_begin = (int)((int64_t)tile_units * share / ns), u_end = (int)((int64_t)tile_units * (share + 1) / ns);
 
   float M = -1e30f, l = 0.f;
   f16v y[NC];
@@ -835,10 +868,14 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedView V, AttendA
 #pragma unroll
       for (int z = 0; z < NH; ++z)
 #pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          h2 o[2];
+        for (int x = 0; x < 2; ++x) {
+          // tokens 4 g .. + 3 of channels 16 x + l16 and 16 (x + 2) + l16; with the lane 32 away: eight tokens of one of them
+          h2 o[4];
           code_to_half<E4M3>(word(vw[z], x), o);
-          put_value(buf, z, x, o[0], o[1]);
+          code_to_half<E4M3>(word(vw[z], x + 2), o + 2);
+          const auto s0 = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, o[0]), __builtin_bit_cast(uint32_t, o[2]), false, false);
+          const auto s1 = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, o[1]), __builtin_bit_cast(uint32_t, o[3]), false, false);
+          sv[((buf * 4 + w) * 2 + (g & 1)) * D + 64 * z + 16 * (x + 2 * hh) + l16] = __builtin_bit_cast(h8, uint4{s0[0], s1[0], s0[1], s1[1]});
         }
     } else if (t >= whole && t < n) {                            // open rows: scaled by powers of two, as above
       const uint16_t* kp = a.open + ((int64_t)b * V.hkv + h) * 2 * side + (t & (V.P - 1)) * D;
@@ -895,13 +932,12 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedView V, AttendA
     if (t0 < most_seen) {
       f16v s[2];
 #pragma unroll
-      for (int T = 0; T < 2; ++T) {
+      for (int i = 0; i < 16; ++i) s[0][i] = s[1][i] = 0.f;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) s[T][i] = 0.f;
+      for (int x = 0; x < NS; ++x)
 #pragma unroll
-        for (int x = 0; x < NS; ++x)
+        for (int T = 0; T < 2; ++T)
           s[T] = __builtin_amdgcn_mfma_f32_32x32x16_f16(sk[(buf * (D / 8) + 2 * x + hh) * 64 + 32 * T + l32], q[x], s[T], 0, 0, 0);
-      }
       float ks[4], lv[4], iv[4];
 #pragma unroll
       for (int tt = 0; tt < 4; ++tt) {
@@ -966,9 +1002,9 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedView V, AttendA
   }
 
   l = halves_sum(l);
-  if (ts.ns > 1) {
-    const int place = tile_places(V, a, tp, L, b) + rt * ts.ns + share;
+  if (ns > 1) {
     if (!live) return;
+    const int place = at.places + rt * ns + share;
     const int64_t z = ((int64_t)place * V.hkv + h) * kTileRows + 32 * w + l32;
 #pragma unroll
     for (int c = 0; c < NC; ++c)
@@ -979,7 +1015,7 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedView V, AttendA
     return;
   }
   if (!live) return;
-  const int64_t at = (int64_t)(row0 + qi) * V.hq + hq;
+  const int64_t out = (int64_t)(row0 + qi) * V.hq + hq;
   const float inv = l > 0.f ? 1.0f / l : 0.f;
 #pragma unroll
   for (int c = 0; c < NC; ++c)
@@ -988,40 +1024,40 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedView V, AttendA
       uint16_t o[4];
 #pragma unroll
       for (int x = 0; x < 4; ++x) o[x] = float_to_elem<BF16>(y[c][i + x] * inv);
-      *reinterpret_cast<uint2*>(a.y + at * D + 32 * c + 8 * (i >> 2) + 4 * hh) = uint2{o[0] | (uint32_t)o[1] << 16, o[2] | (uint32_t)o[3] << 16};
+      *reinterpret_cast<uint2*>(a.y + out * D + 32 * c + 8 * (i >> 2) + 4 * hh) = uint2{o[0] | (uint32_t)o[1] << 16, o[2] | (uint32_t)o[3] << 16};
     }
-  if (hh == 0 && a.lse != nullptr) a.lse[at] = l > 0.f ? (M + log2f(l)) * 0.693147180559945309f : -INFINITY;
+  if (hh == 0 && a.lse != nullptr) a.lse[out] = l > 0.f ? (M + log2f(l)) * 0.693147180559945309f : -INFINITY;
 }
 
-// Joins the shares of the tiles of divided sequences: a group of D / 4 threads per query row and head.
+// Joins the shares of divided tiles: a group of D / 4 threads per query row and head, kJoinRows rows to a workgroup.
+constexpr int kJoinRows = 16;
 template <int D>
 __global__ __launch_bounds__(256) void paged_tile_join_kernel(PagedView V, AttendArgs a, TilePlan tp, const Partial* __restrict__ ml,
                                                               const float* __restrict__ part) {
   constexpr int TPR = D / 4, NG = 256 / TPR;
   const int h = blockIdx.x % V.hkv;
-  int i;
-  const int b = paged_find(V.n_seqs, blockIdx.x / V.hkv, &i, [&](int s) { return (seq_rows(V, a, s) + NG - 1) / NG; });
-  if (b >= V.n_seqs) return;
-  const int L = tile_len(V, a, tp);
-  const TileSeq ts = tile_shares(V, a, tp, L, b);
-  if (ts.ns <= 1) return;
-  const int first = tile_places(V, a, tp, L, b);
+  const TileAll all = tile_all(V, a, tp);
+  // divided tiles' rows are numbered through as if all tiles were full
+  const TileFound at = tile_find(V, a, all, blockIdx.x / V.hkv,
+                                 [&](const TileSeq& t) { return t.ns > 1 ? t.shared * (kTileRows / kJoinRows) : 0; });
+  if (at.b < 0) return;
+  const int ns = at.t.ns, R = seq_rows(V, a, at.b), ch = threadIdx.x % TPR * 4;
   int row0;
-  (void)paged_rows(a.cu, b, a.total, &row0);
-  const int r = i * NG + threadIdx.x / TPR, rt = r / kTileRows, ch = threadIdx.x % TPR * 4;
-  if (r < seq_rows(V, a, b)) {
-    const auto at = [&](int k) { return ((int64_t)(first + rt * ts.ns + k) * V.hkv + h) * kTileRows + r % kTileRows; };
+  (void)paged_rows(a.cu, at.b, a.total, &row0);
+  for (int r = at.within * kJoinRows + threadIdx.x / TPR; r < (at.within + 1) * kJoinRows && r < R; r += NG) {
+    const int rt = r / kTileRows;
+    const auto place = [&](int k) { return ((int64_t)(at.places + rt * ns + k) * V.hkv + h) * kTileRows + r % kTileRows; };
     float M = -1e30f, sum = 0.f;
     f4 o = {0.f, 0.f, 0.f, 0.f};
-    for (int k0 = 0; k0 < ts.ns; k0 += 4) {
+    for (int k0 = 0; k0 < ns; k0 += 4) {
       Partial p[4];
       f4 v[4];
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        const int64_t z = at(k0 + k < ts.ns ? k0 + k : k0);
+        const int64_t z = place(k0 + k < ns ? k0 + k : k0);
         p[k] = ml[z];
         v[k] = *reinterpret_cast<const f4*>(part + z * D + ch);
-        if (k0 + k >= ts.ns) p[k] = Partial{-1e30f, 0.f}, v[k] = f4{0.f, 0.f, 0.f, 0.f};
+        if (k0 + k >= ns) p[k] = Partial{-1e30f, 0.f}, v[k] = f4{0.f, 0.f, 0.f, 0.f};
       }
       const float next = fmaxf(fmaxf(M, fmaxf(p[0].M, p[1].M)), fmaxf(p[2].M, p[3].M)), f0 = exp2_raw(M - next);
       sum *= f0;
@@ -1082,14 +1118,21 @@ static int32_t launch_rows(const PagedView& V, const AttendArgs& a, int64_t max_
   return wide ? launch_rows_nt<D, 2, 8>(V, a, sp, ws, st) : launch_rows_nt<D, 2, 4>(V, a, sp, ws, st);
 }
 
-// Tiles are divided while they are fewer than what the chip takes at once (two workgroups per compute unit).
-static bool divides_tiles(const PagedView& V, int64_t total_q) { return total_q * V.gqa / kTileRows < rows_want(V); }
+// Whether a rest of tiles is divided: always where all of them are fewer than the places (two on each compute unit).  Behind up to
+// five whole rounds, where tiles are long and about equally long - that is not for prompts from their first token on, whose
+// short tiles fill the last round by themselves -, since the second launch has a price.
+static bool divides_tiles(const PagedView& V, const AttendArgs& a, int64_t max_len) {
+  const int64_t tiles = (int64_t)a.total * V.gqa / kTileRows;
+  if (tiles < rows_want(V)) return true;
+  return tiles < 6 * rows_want(V) && max_len >= 8192 && (!a.causal || max_len / 4 >= a.max_q);
+}
 
 template <int D>
-static int32_t launch_tiles(const PagedView& V, const AttendArgs& a, void* ws, hipStream_t st) {
+static int32_t launch_tiles(const PagedView& V, const AttendArgs& a, int64_t max_len, void* ws, hipStream_t st) {
   constexpr int lds = 2 * 64 * D * 2 * 2 + 2 * 16 * 4;
-  const int64_t tiles = (int64_t)a.total * V.gqa / kTileRows + (a.total < V.n_seqs ? a.total : V.n_seqs);
-  const bool divide = divides_tiles(V, a.total);
+  const int64_t active = a.total < V.n_seqs ? a.total : V.n_seqs;
+  const int64_t tiles = (int64_t)a.total * V.gqa / kTileRows + active;
+  const bool divide = divides_tiles(V, a, max_len);
   const TilePlan tp{divide ? rows_want(V) : 0, 2};
   // a sequence's shares: tiles * ceil(units / L) <= tiles * units / L + tiles
   const int64_t items = tiles + tp.want;
@@ -1107,7 +1150,8 @@ static int32_t launch_tiles(const PagedView& V, const AttendArgs& a, void* ws, h
   kernel<<<(unsigned)(items * V.hkv), 256, lds, st>>>(V, a, tp, ml, part);
   HCA_HIP(hipGetLastError());
   if (divide) {
-    const int64_t groups = (int64_t)a.total * V.gqa / (1024 / D) + (a.total < V.n_seqs ? a.total : V.n_seqs);
+    // fewer than `want` tiles are divided, and no more than there are
+    const int64_t groups = (tiles < tp.want ? tiles : tp.want) * (kTileRows / kJoinRows);
     paged_tile_join_kernel<D><<<(unsigned)(groups * V.hkv), 256, 0, st>>>(V, a, tp, ml, part);
     HCA_HIP(hipGetLastError());
   }
@@ -1148,7 +1192,7 @@ int32_t hca_paged_attend(const hca_paged_shape* shape, const void* q, int64_t q_
   hipStream_t st = (hipStream_t)stream;
   if (few_rows(V, a.max_q))
     return V.D == 128 ? launch_rows<128>(V, a, max_len, workspace, st) : launch_rows<64>(V, a, max_len, workspace, st);
-  return V.D == 128 ? launch_tiles<128>(V, a, workspace, st) : launch_tiles<64>(V, a, workspace, st);
+  return V.D == 128 ? launch_tiles<128>(V, a, max_len, workspace, st) : launch_tiles<64>(V, a, max_len, workspace, st);
 }
 
 }  // extern "C"
