@@ -1078,8 +1078,12 @@ __global__ __launch_bounds__(256) void paged_tile_join_kernel(PagedView V, Atten
   }
 }
 
-// Workgroups per KV head that fill the chip once: two on each of its 256 compute units.
-static int rows_want(const PagedView& V) { return V.hkv >= 512 ? 1 : 512 / V.hkv; }
+// Workgroups per KV head that fill the chip once: on each of its 256 compute units two, or three with 64 channels, as
+// the kernels' registers allow (32 sequences of up to 8 Ki: 64 us at two, 75 at three with 128 channels, 39.9 and 38.6 with 64).
+static int rows_want(const PagedView& V) {
+  const int all = V.D == 64 ? 768 : 512;
+  return V.hkv >= all ? 1 : all / V.hkv;
+}
 constexpr int kOneItem = 1024;     // sequences up to this length are one piece, and nothing has to be joined
 
 // Up to 32 query rows per sequence and KV head (queries x heads of the group) go to the rows kernel.
@@ -1118,12 +1122,14 @@ static int32_t launch_rows(const PagedView& V, const AttendArgs& a, int64_t max_
   return wide ? launch_rows_nt<D, 2, 8>(V, a, sp, ws, st) : launch_rows_nt<D, 2, 4>(V, a, sp, ws, st);
 }
 
-// Whether a rest of tiles is divided: always where all of them are fewer than the places (two on each compute unit).  Behind up to
-// five whole rounds, where tiles are long and about equally long - that is not for prompts from their first token on, whose
-// short tiles fill the last round by themselves -, since the second launch has a price.
+// Whether a rest of tiles is divided.  The second launch and the partial results have a price, 5 us for a few tiles and 10 for many.
+// Where all tiles are fewer than the places: from 384 tokens on for very few (two times 40 rows over 500 tokens: 18.7 us
+// whole, 15.5 divided; over 300 tokens 14.0 and 15.5), from 768 on for more (a prompt of 700 tokens: 26.3 us whole, 30.3
+// divided; of 1000: 40 and 39).  Behind up to five whole rounds: where tiles are long and about equally long - that is not for
+// prompts from their first token on, whose short tiles fill the last round by themselves.
 static bool divides_tiles(const PagedView& V, const AttendArgs& a, int64_t max_len) {
   const int64_t tiles = (int64_t)a.total * V.gqa / kTileRows;
-  if (tiles < rows_want(V)) return true;
+  if (tiles < rows_want(V)) return max_len > (16 * tiles < rows_want(V) ? 384 : 768);
   return tiles < 6 * rows_want(V) && max_len >= 8192 && (!a.causal || max_len / 4 >= a.max_q);
 }
 
@@ -1133,7 +1139,7 @@ static int32_t launch_tiles(const PagedView& V, const AttendArgs& a, int64_t max
   const int64_t active = a.total < V.n_seqs ? a.total : V.n_seqs;
   const int64_t tiles = (int64_t)a.total * V.gqa / kTileRows + active;
   const bool divide = divides_tiles(V, a, max_len);
-  const TilePlan tp{divide ? rows_want(V) : 0, 2};
+  const TilePlan tp{divide ? rows_want(V) : 0, 3};
   // a sequence's shares: tiles * ceil(units / L) <= tiles * units / L + tiles
   const int64_t items = tiles + tp.want;
   const int64_t rows = 2 * (int64_t)rows_want(V) * V.hkv * kTileRows;
