@@ -597,9 +597,11 @@ int32_t hca_vq_evict(const hca_shape* shape, const hca_vq_codebook* cb, void* pc
  *             values  [P/16][head_dim/64][4 g][16 c][4 u][4 j]  token 4 g + j of the tile, channel 64 * second + 16 u + c
  *   scale   fp32 [n_pages, n_kv_heads, 2]
  *   open    elem [n_seqs, n_kv_heads, 2, P * head_dim]: rows in the same tiles
- * kv, scale and open need no initial values; kv, open and rows of new keys, values and queries are 16-byte aligned.
+ * kv, scale and open need no initial values; kv, open and rows of new keys, values and queries are 16-byte aligned, scale
+ * is 8-byte aligned.
  * Supported: head_dim 64 or 128; page 16, 32, 64 or 128; n_q_heads / n_kv_heads 1 .. 16; up to 1024 sequences of up to 2^30
- * tokens, 2^37 in all rows of the table together; n_pages * page below 2^31.  Anything else: HCA_ERR_UNSUPPORTED. */
+ * tokens, 2^37 in all rows of the table together; n_pages * page below 2^31; calls of up to 2^27 new rows and 2^22 query
+ * rows (fewer where total_q * n_q_heads comes near 2^31).  Anything else: HCA_ERR_UNSUPPORTED. */
 #define HCA_F16 0      /* elem: IEEE half */
 #define HCA_BF16 1     /* elem: bfloat16 */
 #define HCA_INT8 0     /* code: signed integers -127 .. 127 */

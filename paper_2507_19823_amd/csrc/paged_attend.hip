@@ -16,7 +16,6 @@ struct AttendArgs {
   float* lse;
 };
 
-
 typedef _Float16 h2 __attribute__((ext_vector_type(2)));
 typedef _Float16 h4 __attribute__((ext_vector_type(4)));
 typedef _Float16 h8 __attribute__((ext_vector_type(8)));
@@ -234,7 +233,7 @@ struct Partial {          // of one item, KV head and row: reference, sum; the w
 
 template <int D, int NT, int NW, bool BF16, bool E4M3>
 __global__ __launch_bounds__(64 * NW, 2) void paged_rows_kernel(PagedView V, AttendArgs a, SplitPlan sp,
-                                                                          Partial* __restrict__ ml, float* __restrict__ part) {
+                                                                Partial* __restrict__ ml, float* __restrict__ part) {
   constexpr int NH = D / 64, NC = D / 16, COLS = 16 * NT;
   constexpr int TT = NT == 1 ? 4 : 2, STEP = 16 * TT;  // tiles and tokens that a wave works on at a time
   extern __shared__ float lds[];                       // [NW][COLS][D + 4], then M and l of each wave [NW][COLS]
@@ -1190,8 +1189,11 @@ int32_t hca_paged_attend(const hca_paged_shape* shape, const void* q, int64_t q_
     return HCA_ERR_BAD_ARG;
   if (!(sm_scale > 0.0f)) return HCA_ERR_BAD_ARG;
   if (q_stride < (int64_t)V.hq * V.D || q_stride % 8 != 0) return HCA_ERR_BAD_ARG;
-  if (!aligned16(q) || !aligned16(y) || !aligned16(kv) || !aligned16(open) || ((uintptr_t)workspace & 255) != 0) return HCA_ERR_BAD_ARG;
-  if (total_q > (int64_t)1 << 26) return HCA_ERR_UNSUPPORTED;
+  if (!aligned16(q) || !aligned16(y) || !aligned16(kv) || !aligned16(open) || ((uintptr_t)scale & 7) != 0 ||
+      ((uintptr_t)workspace & 255) != 0)
+    return HCA_ERR_BAD_ARG;
+  // a launch has fewer than 2^32 threads along x: 2^24 workgroups
+  if (total_q > (int64_t)1 << 22 || total_q * V.hq / kTileRows + (int64_t)2048 * V.hkv >= (int64_t)1 << 24) return HCA_ERR_UNSUPPORTED;
   if (total_q == 0 || max_q == 0) return HCA_OK;
   const AttendArgs a{(const uint16_t*)q, q_stride, cu, lens, tables, (const uint8_t*)kv, scale, (const uint16_t*)open,
                      sm_scale * 1.44269504088896341f, (int32_t)total_q, (int32_t)(max_q < total_q ? max_q : total_q), causal, (uint16_t*)y, lse};

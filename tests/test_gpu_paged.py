@@ -278,6 +278,68 @@ def test_attend_many_sequences(B):
     rig.attend(rig.rows(200, 4, 64), list(range(201)))
 
 
+@pytest.mark.parametrize("q,hq", [(1, 4), (6, 8), (20, 4)])
+def test_attend_ranges_across_many_sequences(B, q, hq):
+    """More than 64 sequences, the caller expecting long ones: ranges of tokens that span several sequences, and pieces."""
+    lens = [(61 * i) % 523 for i in range(90)]
+    lens[40], lens[70] = 3000, 1500
+    rig = filled(B, lens, hq, 2, 64, 32, "f16", "int8", seed=q)
+    m = [0 if i % 7 == 3 else min(q, 1 + i % q) for i in range(90)]
+    cu = [0]
+    for t in m:
+        cu.append(cu[-1] + t)
+    rig.attend(rig.rows(cu[-1], hq, 64), cu, max_q=q, max_len=1 << 20)
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("hkv,m", [(128, [400, 0, 530, 77]), (256, [130, 260, 5, 300]), (64, [70, 64, 200, 300])])
+def test_attend_whole_tiles_and_a_divided_rest(B, hkv, m, causal):
+    """So many KV heads that a round has 8, 4 or 2 tiles per head: whole rounds of tiles, and shares of the rest, joined."""
+    lens = [max(t, 90) + 60 * i for i, t in enumerate(m)]
+    rig = filled(B, lens, hkv, hkv, 64, 32, "bf16", "e4m3", seed=hkv)
+    cu = [0]
+    for t in m:
+        cu.append(cu[-1] + t)
+    rig.attend(rig.rows(cu[-1], hkv, 64), cu, causal=causal, max_len=1 << 20)
+
+
+def test_pages_beyond_four_gigabytes(B):
+    """The same sequence in the last pages of a cache of 5 GB and in a small one: the same bits."""
+    n, P, hkv = 700, 128, 8
+    out = []
+    for n_pages, first in ((20000, 19994), (8, 2)):
+        shape = B.make_paged_shape(1, 32, hkv, P, n_pages, 6, 128, "f16", "int8")
+        g = torch.Generator(device="cuda").manual_seed(1)
+        k, v = (torch.randn(n, hkv, 128, generator=g, device="cuda").half() for _ in range(2))
+        q = torch.randn(70, 32, 128, generator=g, device="cuda").half()
+        kv = torch.empty(B.hca_paged_cache_bytes(shape), dtype=torch.uint8, device="cuda")
+        scale = torch.empty(n_pages, hkv, 2, device="cuda")
+        op = torch.empty(B.hca_paged_open_bytes(shape) // 2, dtype=torch.float16, device="cuda")
+        tables = dev([[first + i for i in range(6)]])
+        B.hca_paged_store(shape, k, 1024, v, 1024, n, dev([0]), dev([0, n]), tables, kv, scale, op)
+        for m in (1, 70):
+            y, lse = torch.zeros(m, 32, 128, dtype=torch.float16, device="cuda"), torch.zeros(m, 32, device="cuda")
+            ws = torch.empty(B.hca_paged_workspace_bytes(shape, m, m), dtype=torch.uint8, device="cuda")
+            B.hca_paged_attend(shape, q, 4096, dev([0, m]), m, m, dev([n]), n, tables, kv, scale, op, 0.09, True, y, lse, ws)
+            out.append((y.cpu(), lse.cpu()))
+        del kv
+    assert torch.isfinite(out[0][0]).all() and out[0][0].float().abs().max() > 0
+    for a, b in zip(out[:2], out[2:]):
+        assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+def test_slots_up_to_the_largest_number(B):
+    n_pages = (2 ** 31 - 1) // 128
+    shape = B.make_paged_shape(1, 1, 1, 128, n_pages, 3)
+    fr = torch.zeros(n_pages, dtype=torch.int32, device="cuda")
+    fr[:3] = dev([5, n_pages - 2, n_pages - 1])
+    tables, lens, cnt, start, cu = dev([[-1] * 3]), dev([0]), dev([3]), dev([0]), dev([0, 0])
+    tok = torch.zeros(3, 300, dtype=torch.int32, device="cuda")
+    B.hca_paged_map(shape, dev([300]), lens, lens, tables, fr, cnt, cnt, 300, start, cu, tok[0], tok[1], tok[2])
+    assert tables.tolist() == [[n_pages - 1, n_pages - 2, 5]]
+    assert tok[2, :128].tolist() == [(n_pages - 1) * 128 + i for i in range(128)] and tok[2, 299].item() == 5 * 128 + 43
+
+
 def test_attend_weights_of_one_sharp_peak_and_of_a_flat_row(B):
     """Scores far apart (all weight on one token, the running maximum moving late) and all equal."""
     rig = filled(B, [700, 700], 4, 1, 128, 32, "f16", "e4m3", seed=4)

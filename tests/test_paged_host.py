@@ -79,7 +79,7 @@ def test_store_refuses(B):
         assert rc(**{n: odd}) == -1, n
     for n in ("ks", "vs"):
         assert rc(**{n: 1016}) == -1 and rc(**{n: 1028}) == -1, n      # shorter than a row; no multiple of 8
-    assert rc(total=-1) == -1 and rc(total=2 ** 30 + 1) == -2
+    assert rc(total=-1) == -1 and rc(total=2 ** 27 + 1) == -2
     assert rc(total=0, k=None, v=None) == 0                            # nothing to do, nothing launched
 
 
@@ -98,5 +98,6 @@ def test_attend_refuses(B):
     assert rc(qs=4088) == -1 and rc(qs=4100) == -1
     assert rc(sm=0.0) == -1 and rc(sm=-1.0) == -1 and rc(sm=float("nan")) == -1
     assert rc(total=-1) == -1 and rc(max_q=-1) == -1 and rc(max_len=-1) == -1
-    assert rc(total=2 ** 26 + 1) == -2
+    assert rc(total=2 ** 26 + 1) == -2 and rc(total=2 ** 22 + 1) == -2
+    assert rc(scale=C.c_void_p(260)) == -1
     assert rc(total=0, q=None, y=None) == 0 and rc(max_q=0) == 0
