@@ -686,6 +686,7 @@ constexpr int kTileRows = 128;
 struct TilePlan {
   int32_t want;         // places per KV head; 0: all tiles go out whole
   int32_t least;        // units per share at least
+  int32_t join;         // rows per workgroup of the second launch
 };
 struct TileSeq { int tiles, units, shared, ns; };       // `shared` of the tiles, the ones that see least, go out in ns shares each
 __device__ __forceinline__ TileSeq tile_seq(const PagedView& V, const AttendArgs& a, int b) {
@@ -1028,8 +1029,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void paged_tile_kernel(PagedV
   if (hh == 0 && a.lse != nullptr) a.lse[out] = l > 0.f ? (M + log2f(l)) * 0.693147180559945309f : -INFINITY;
 }
 
-// Joins the shares of divided tiles: a group of D / 4 threads per query row and head, kJoinRows rows to a workgroup.
-constexpr int kJoinRows = 16;
+// Joins the shares of divided tiles: a group of D / 4 threads per query row and head, tp.join rows to a workgroup.
 template <int D>
 __global__ __launch_bounds__(256) void paged_tile_join_kernel(PagedView V, AttendArgs a, TilePlan tp, const Partial* __restrict__ ml,
                                                               const float* __restrict__ part) {
@@ -1038,12 +1038,12 @@ __global__ __launch_bounds__(256) void paged_tile_join_kernel(PagedView V, Atten
   const TileAll all = tile_all(V, a, tp);
   // divided tiles' rows are numbered through as if all tiles were full
   const TileFound at = tile_find(V, a, all, blockIdx.x / V.hkv,
-                                 [&](const TileSeq& t) { return t.ns > 1 ? t.shared * (kTileRows / kJoinRows) : 0; });
+                                 [&](const TileSeq& t) { return t.ns > 1 ? t.shared * (kTileRows / tp.join) : 0; });
   if (at.b < 0) return;
   const int ns = at.t.ns, R = seq_rows(V, a, at.b), ch = threadIdx.x % TPR * 4;
   int row0;
   (void)paged_rows(a.cu, at.b, a.total, &row0);
-  for (int r = at.within * kJoinRows + threadIdx.x / TPR; r < (at.within + 1) * kJoinRows && r < R; r += NG) {
+  for (int r = at.within * tp.join + threadIdx.x / TPR; r < (at.within + 1) * tp.join && r < R; r += NG) {
     const int rt = r / kTileRows;
     const auto place = [&](int k) { return ((int64_t)(at.places + rt * ns + k) * V.hkv + h) * kTileRows + r % kTileRows; };
     float M = -1e30f, sum = 0.f;
@@ -1138,7 +1138,8 @@ static int32_t launch_tiles(const PagedView& V, const AttendArgs& a, int64_t max
   const int64_t active = a.total < V.n_seqs ? a.total : V.n_seqs;
   const int64_t tiles = (int64_t)a.total * V.gqa / kTileRows + active;
   const bool divide = divides_tiles(V, a, max_len);
-  const TilePlan tp{divide ? rows_want(V) : 0, 3};
+  // behind whole rounds the rest is mostly small: few workgroups to find that there is nothing to join
+  const TilePlan tp{divide ? rows_want(V) : 0, 3, tiles < rows_want(V) ? 16 : 64};
   // a sequence's shares: tiles * ceil(units / L) <= tiles * units / L + tiles
   const int64_t items = tiles + tp.want;
   const int64_t rows = 2 * (int64_t)rows_want(V) * V.hkv * kTileRows;
@@ -1156,7 +1157,7 @@ static int32_t launch_tiles(const PagedView& V, const AttendArgs& a, int64_t max
   HCA_HIP(hipGetLastError());
   if (divide) {
     // fewer than `want` tiles are divided, and no more than there are
-    const int64_t groups = (tiles < tp.want ? tiles : tp.want) * (kTileRows / kJoinRows);
+    const int64_t groups = (tiles < tp.want ? tiles : tp.want) * (kTileRows / tp.join);
     paged_tile_join_kernel<D><<<(unsigned)(groups * V.hkv), 256, 0, st>>>(V, a, tp, ml, part);
     HCA_HIP(hipGetLastError());
   }
