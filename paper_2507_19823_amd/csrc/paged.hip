@@ -246,9 +246,9 @@ __global__ __launch_bounds__(256) void paged_store_kernel(PagedView V, StoreArgs
   constexpr int RS = D + 8, PT = D / 16 * 16;   // row stride in LDS, pieces per tile of 16 tokens
   extern __shared__ uint16_t rows[];            // [P][RS]
   __shared__ uint32_t wmax[4];
-  const int h = blockIdx.y, side = blockIdx.z, tid = threadIdx.x;
+  const int side = blockIdx.x & 1, h = (blockIdx.x >> 1) % V.hkv, tid = threadIdx.x;      // a token's heads and sides side by side
   int m;
-  const int b = paged_find(V.n_seqs, blockIdx.x, &m, [&](int s) { return store_items(V, a, s); });
+  const int b = paged_find(V.n_seqs, (int)((blockIdx.x >> 1) / V.hkv), &m, [&](int s) { return store_items(V, a, s); });
   if (b >= V.n_seqs) return;
   int row0;
   const int T = paged_rows(a.cu, b, a.total, &row0), start = a.start[b];
@@ -360,7 +360,7 @@ __global__ __launch_bounds__(256) void paged_store_kernel(PagedView V, StoreArgs
 }
 
 template <int D, bool BF16>
-static int32_t launch_store(const PagedView& V, const StoreArgs& a, dim3 grid, hipStream_t st) {
+static int32_t launch_store(const PagedView& V, const StoreArgs& a, unsigned grid, hipStream_t st) {
   const int lds = V.P * (D + 8) * 2;
   if (V.code == HCA_E4M3)
     paged_store_kernel<D, BF16, true><<<grid, 256, lds, st>>>(V, a);
@@ -428,13 +428,14 @@ int32_t hca_paged_store(const hca_paged_shape* shape, const void* k, int64_t k_s
   const int64_t least = (int64_t)V.hkv * V.D;
   if (k_stride < least || v_stride < least || k_stride % 8 != 0 || v_stride % 8 != 0) return HCA_ERR_BAD_ARG;
   if (!aligned16(k) || !aligned16(v) || !aligned16(kv) || !aligned16(open)) return HCA_ERR_BAD_ARG;
-  if (total > (int64_t)1 << 27) return HCA_ERR_UNSUPPORTED;      // a launch has fewer than 2^32 threads along x
+  if (total > (int64_t)1 << 27) return HCA_ERR_UNSUPPORTED;
   if (total == 0) return HCA_OK;
   const StoreArgs a{{(const uint16_t*)k, (const uint16_t*)v}, {k_stride, v_stride}, (int32_t)total, start, cu, tables,
                     (uint8_t*)kv, scale, (uint16_t*)open};
   // a sequence with T rows has at most (T + P - 1) / P <= T / P + 1 items
   const int64_t items = total / V.P + (total < V.n_seqs ? total : V.n_seqs);
-  const dim3 grid((unsigned)items, (unsigned)V.hkv, 2);
+  if (items * V.hkv * 2 >= (int64_t)1 << 24) return HCA_ERR_UNSUPPORTED;      // a launch has fewer than 2^32 threads along x
+  const unsigned grid = (unsigned)(items * V.hkv * 2);
   hipStream_t st = (hipStream_t)stream;
   if (V.D == 128) return V.elem == HCA_BF16 ? launch_store<128, true>(V, a, grid, st) : launch_store<128, false>(V, a, grid, st);
   return V.elem == HCA_BF16 ? launch_store<64, true>(V, a, grid, st) : launch_store<64, false>(V, a, grid, st);
