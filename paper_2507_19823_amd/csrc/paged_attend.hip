@@ -172,7 +172,10 @@ __device__ __forceinline__ float largest(const uint4& raw) {
 // are numbered through, workgroup i takes units [i C, (i + 1) C), which may be the end of one sequence, some whole ones and
 // the beginning of another.  At most two of its pieces are not whole sequences: they go to its two places in the
 // workspace, and a second launch joins them.  (Items of one sequence each, of at most L units, left a short item behind
-// most sequences and a second round of workgroups: 32 sequences of 2.5 to 8 Ki took 83 us where this takes 61.)
+// most sequences and a second round of workgroups: 32 sequences of 2.5 to 8 Ki took 83 us where this takes 59.)  Where the
+// ranges would be short, fewer than kShort units, a second piece costs a workgroup more (5 us of waiting for its first
+// loads) than an uneven division: then each sequence is cut into equal shares, a workgroup each (eight sequences of 3000 tokens:
+// 20.8 and 18.3 us), if they fit.
 constexpr int kUnit = 64;
 
 struct SplitPlan {
@@ -205,15 +208,35 @@ __device__ __forceinline__ Seq seq_of_lane(const Seq& s, int l) {
   return Seq{__builtin_amdgcn_readlane(s.row0, l), __builtin_amdgcn_readlane(s.m, l), __builtin_amdgcn_readlane(s.n, l),
              __builtin_amdgcn_readlane(s.units, l)};
 }
-// units per workgroup (all units together are fewer than 2^31: see paged_view)
-__device__ __forceinline__ int split_len(const SplitPlan& sp, uint32_t all) {
-  const int C = (int)((all + (uint32_t)sp.want - 1) / (uint32_t)sp.want);
-  return C > sp.least ? C : sp.least;
+constexpr int kShort = 32;
+struct Split {
+  int C;                // units per workgroup at most
+  bool shares;          // each sequence in equal shares of at most C units; else ranges of C units across sequences
+  __device__ int count(int units) const { return shares ? (units + C - 1) / C : units; }     // what is numbered through
+};
+// All units together are fewer than 2^31 (see paged_view).  items(C): workgroups that shares of up to C units take.
+template <typename F>
+__device__ __forceinline__ Split split_of(const SplitPlan& sp, uint32_t all, F&& items) {
+  int C = (int)((all + (uint32_t)sp.want - 1) / (uint32_t)sp.want);
+  if (C < sp.least) C = sp.least;
+  if (C < kShort)
+    for (int x = C; x < C + 4; ++x)
+      if (items(x) <= (uint32_t)sp.want) return Split{x, true};
+  return Split{C, false};
 }
-__device__ __forceinline__ uint32_t all_units(const PagedView& V, const AttendArgs& a) {
-  uint32_t units = 0;
-  for (int b = threadIdx.x & 63; b < V.n_seqs; b += 64) units += (uint32_t)seq_units(V, a, b);
-  return wave_sum(units);
+// mine: sequence `lane`, which callers have read already
+__device__ __forceinline__ Split split_all(const PagedView& V, const AttendArgs& a, const SplitPlan& sp, const Seq& mine, uint32_t* all) {
+  const auto sum = [&](auto&& f) {
+    uint32_t x = (uint32_t)f(mine.units);
+    for (int b = 64 + (threadIdx.x & 63); b < V.n_seqs; b += 64) x += (uint32_t)f(seq_units(V, a, b));
+    return wave_sum(x);
+  };
+  *all = sum([](int u) { return u; });
+  if (__popcll(__ballot(mine.units > 0)) <= 1 && V.n_seqs <= 64) {       // one sequence: ranges are shares
+    const int C = (int)((*all + (uint32_t)sp.want - 1) / (uint32_t)sp.want);
+    return Split{C > sp.least ? C : sp.least, false};
+  }
+  return split_of(sp, *all, [&](int C) { return sum([&](int u) { return (u + C - 1) / C; }); });
 }
 
 // Four channels of output row `at` from the weighted values, the reference and the sum of the weights.
@@ -243,35 +266,41 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_rows_kernel(PagedView V, Att
   const int64_t side = V.side();
 
   // the workgroup's piece: from unit u of sequence b on, `left` units.  Up to 64 sequences: their lengths are read once.
-  int b, u, left;
+  int b, u, left = 0;
   Seq sq;
-  const auto whole_seqs = [&](int units) { return sp.want == 0 ? (units > 0 ? 1 : 0) : units; };
+  Split cut{1, false};
+  const auto numbered = [&](int units) { return sp.want == 0 ? (units > 0 ? 1 : 0) : cut.count(units); };
+  const auto range = [&](uint32_t all) {                        // of the numbering: false if there is nothing for this workgroup
+    const int64_t U0 = (int64_t)blockIdx.x * cut.C;
+    left = all - U0 < cut.C ? (int)(all - U0) : cut.C;
+    return U0 < all;
+  };
+  Seq mine{0, 0, 0, 0};
+  if (lane < V.n_seqs) mine = seq_info(V, a, lane);
+  if (sp.want != 0) {
+    uint32_t all;
+    cut = split_all(V, a, sp, mine, &all);
+    if (!cut.shares && !range(all)) return;
+  }
+  const int i = sp.want == 0 || cut.shares ? (int)blockIdx.x : (int)blockIdx.x * cut.C;
   if (V.n_seqs <= 64) {
-    Seq mine{0, 0, 0, 0};
-    if (lane < V.n_seqs) mine = seq_info(V, a, lane);
-    const int c = whole_seqs(mine.units);
-    const uint32_t incl = wave_scan_incl((uint32_t)c), all = wave_last(incl);
-    const int C = sp.want == 0 ? 1 : split_len(sp, all);
-    const int64_t U0 = (int64_t)blockIdx.x * C;
-    if (U0 >= all) return;
-    left = all - U0 < C ? (int)(all - U0) : C;
-    const int l = __builtin_ctzll(__ballot(incl > (uint32_t)U0));
+    const int c = numbered(mine.units);
+    const uint32_t incl = wave_scan_incl((uint32_t)c);
+    const uint64_t past = __ballot(incl > (uint32_t)i);
+    if (past == 0) return;
+    const int l = __builtin_ctzll(past);
     b = l;
-    u = (int)U0 - (__builtin_amdgcn_readlane((int)incl, l) - __builtin_amdgcn_readlane(c, l));
+    u = i - (__builtin_amdgcn_readlane((int)incl, l) - __builtin_amdgcn_readlane(c, l));
     sq = seq_of_lane(mine, l);
   } else {
-    int C = 1;
-    uint32_t all = 0xffffffffu;
-    if (sp.want != 0) {
-      all = all_units(V, a);
-      C = split_len(sp, all);
-    }
-    const int64_t U0 = (int64_t)blockIdx.x * C;
-    if (U0 >= all) return;
-    left = all - U0 < C ? (int)(all - U0) : C;
-    b = paged_find(V.n_seqs, (int)U0, &u, [&](int x) { return whole_seqs(seq_units(V, a, x)); });
+    b = paged_find(V.n_seqs, i, &u, [&](int x) { return numbered(seq_units(V, a, x)); });
     if (b >= V.n_seqs) return;
     sq = seq_info(V, a, b);
+  }
+  if (cut.shares) {
+    const int count = cut.count(sq.units), share = u;
+    u = (int)((int64_t)sq.units * share / count);
+    left = (int)((int64_t)sq.units * (share + 1) / count) - u;
   }
   if (sp.want == 0) left = sq.units;
 
@@ -578,30 +607,27 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedView V, AttendArgs
   __shared__ f4 s_o[NG][TPR];
   __shared__ Partial s_ml[NG];
   const int hq = blockIdx.y, h = hq / V.gqa, lane = threadIdx.x & 63, t = blockIdx.x;
-  // the row's sequence b, query i, and the units before and in it
-  int b = -1, i = 0, S = 0, E = 0;
-  uint32_t all = 0;
-  for (int b0 = 0; b0 < V.n_seqs; b0 += 64) {
-    const int s = b0 + lane;
-    int f = 0, m = 0;
-    uint32_t c = 0;
-    if (s < V.n_seqs) {
-      m = paged_rows(a.cu, s, a.total, &f);
-      c = (uint32_t)seq_units(V, a, s);
-    }
-    const uint32_t incl = wave_scan_incl(c);
-    const uint64_t mine = __ballot(m > 0 && t >= f && t < f + m);
-    if (b < 0 && mine != 0) {
-      const int l = __builtin_ctzll(mine);
+  Seq mine{0, 0, 0, 0};
+  if (lane < V.n_seqs) mine = seq_info(V, a, lane);
+  uint32_t all;
+  const Split cut = split_all(V, a, sp, mine, &all);
+  // the row's sequence b, query i, and the numbers before and up to it
+  int b = -1, i = 0, S = 0, E = 0, before = 0;
+  for (int b0 = 0; b0 < V.n_seqs && b < 0; b0 += 64) {
+    if (b0 > 0) mine = b0 + lane < V.n_seqs ? seq_info(V, a, b0 + lane) : Seq{0, 0, 0, 0};
+    const uint32_t c = (uint32_t)cut.count(mine.units), incl = wave_scan_incl(c);
+    const uint64_t past = __ballot(mine.m > 0 && t >= mine.row0 && t < mine.row0 + mine.m);
+    if (past != 0) {
+      const int l = __builtin_ctzll(past);
       b = b0 + l;
-      i = t - __builtin_amdgcn_readlane(f, l);
-      E = (int)(all + (uint32_t)__builtin_amdgcn_readlane((int)incl, l));
+      i = t - __builtin_amdgcn_readlane(mine.row0, l);
+      E = before + __builtin_amdgcn_readlane((int)incl, l);
       S = E - __builtin_amdgcn_readlane((int)c, l);
     }
-    all += wave_last(incl);
+    before += (int)wave_last(incl);
   }
   if (b < 0 || i >= a.max_q) return;
-  const int C = split_len(sp, all);
+  const int C = cut.shares ? 1 : cut.C;
   const int i0 = S / C, count = (E - 1) / C - i0 + 1;                    // its workgroups
   if (count <= 1) return;
   const int r = i * V.gqa + hq % V.gqa;
