@@ -291,6 +291,19 @@ def test_attend_ranges_across_many_sequences(B, q, hq):
     rig.attend(rig.rows(cu[-1], hq, 64), cu, max_q=q, max_len=1 << 20)
 
 
+@pytest.mark.parametrize("n_seqs,hkv,D,q", [(20, 128, 64, 1), (90, 64, 128, 1), (70, 128, 64, 3), (9, 256, 128, 2)])
+def test_attend_few_ranges_over_many_sequences(B, n_seqs, hkv, D, q):
+    """So many KV heads that there are two to eight ranges per head: each spans sequences, whole ones among them."""
+    lens = [(89 * i) % 400 for i in range(n_seqs)]
+    lens[n_seqs // 2] = 1200
+    rig = filled(B, lens, hkv, hkv, D, 32, "bf16", "int8", seed=n_seqs)
+    m = [0 if i % 8 == 5 else 1 + i % q for i in range(n_seqs)]
+    cu = [0]
+    for t in m:
+        cu.append(cu[-1] + t)
+    rig.attend(rig.rows(cu[-1], hkv, D), cu, max_q=q, max_len=1 << 20)
+
+
 @pytest.mark.parametrize("causal", [True, False])
 @pytest.mark.parametrize("hkv,m", [(128, [400, 0, 530, 77]), (256, [130, 260, 5, 300]), (64, [70, 64, 200, 300])])
 def test_attend_whole_tiles_and_a_divided_rest(B, hkv, m, causal):
