@@ -585,7 +585,9 @@ int32_t hca_vq_evict(const hca_shape* shape, const hca_vq_codebook* cb, void* pc
  *   amax  = largest magnitude of the block's P * head_dim numbers of one KV head and side
  *   scale = max(fp32(amax / m), 2^-64), m = 127 (int8) or 448 (e4m3); inv = fp32(1 / scale)
  *   code  = x * inv (fp32), clamped to [-m, m], rounded to nearest, ties to even
- * so the codes do not depend on how a sequence was cut into calls, and no number is rounded twice.
+ * so the codes do not depend on how a sequence was cut into calls, and no number is rounded twice.  A block in which an
+ * infinity or a NaN is stored gets NaN as its scale: queries that see a token of it get NaN in that head's outputs (in the
+ * open rows, of which 16 count together, a NaN does the same), queries that see none of it are not affected.
  *
  * All lengths, tables and counts are device memory: nothing is read back, and calls can be captured and replayed while
  * lengths change.  What a kernel reads from them is checked there: a page number outside [0, n_pages) holds no tokens

@@ -320,8 +320,9 @@ __global__ __launch_bounds__(256) void paged_store_kernel(PagedView V, StoreArgs
     uint32_t bits = wmax[0];
 #pragma unroll
     for (int k = 1; k < 4; ++k) bits = wmax[k] > bits ? wmax[k] : bits;
-    float scale = elem_to_float<BF16>(bits) / (E4M3 ? 448.f : 127.f);
-    if (!(scale >= 0x1p-64f)) scale = 0x1p-64f;
+    // an infinity or a NaN is seen by its bits, the largest there are: the block gets no scale, so that attention shows it
+    float scale = bits >= (BF16 ? 0x7f80u : 0x7c00u) ? NAN : elem_to_float<BF16>(bits) / (E4M3 ? 448.f : 127.f);
+    if (scale < 0x1p-64f) scale = 0x1p-64f;
     const float inv = 1.0f / scale;
     if (page >= 0 && page < V.n_pages) {
       uint4* out = reinterpret_cast<uint4*>(a.kv + (((int64_t)page * V.hkv + h) * 2 + side) * V.side());

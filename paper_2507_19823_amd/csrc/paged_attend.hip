@@ -25,6 +25,10 @@ __device__ __forceinline__ float exp2_raw(float x) { return __builtin_amdgcn_exp
 __device__ __forceinline__ float log2_raw(float x) { return __builtin_amdgcn_logf(x); }
 __device__ __forceinline__ float lane_value(float v, int l) { return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(v), l)); }
 
+// 1 / scale of a block's values, by which sums of weights are multiplied.  A block with an infinity or a NaN has NaN as its scale: then 0,
+// so that it stays out of the sums of queries that do not see it (those that do get the NaN through its logarithm).
+__device__ __forceinline__ float inverse_scale(float s) { return fmaxf(1.0f / s, 0.f); }
+
 // Four codes as four halves, exactly: an e4m3 number is a half, and so is an integer up to 127 (1024 + u in the
 // mantissa's last bits, minus 1152, u = code + 128).
 template <bool E4M3> __device__ __forceinline__ void code_to_half(uint32_t w, h2* x) {
@@ -60,7 +64,9 @@ __device__ __forceinline__ float rows_sum(float x) {
 // A tile of open rows (16 numbers per lane and 64 channels, as stored) as halves, brought into their range by a power of two:
 // bfloat16 keys to the top of it (below that nothing is lost that counts), values to that of codes, so that their weights
 // are no smaller than a whole page's.  Rows from token n on may hold anything: a key row stays in its own column of the
-// scores, which is masked, so it only must not decide the power; value rows are cleared.  Returns the exponent.
+// scores, which is masked, so it only must not decide the power; value rows are cleared.  Returns the exponent.  A tile with an
+// infinity or a NaN among its values counts as zeros of scale NaN: a weight of 0 would still make a NaN of it in the product,
+// for queries that do not see the token.
 template <int NH, bool BF16>
 __device__ __forceinline__ int open_keys(const uint4 (&raw)[NH][2], bool live, h8 (&o)[NH][2]) {
   if (!BF16) {
@@ -93,9 +99,9 @@ __device__ __forceinline__ int open_keys(const uint4 (&raw)[NH][2], bool live, h
       }
   return ex;
 }
-// first: the token of the lane's numbers 0, 4, 8 and 12 (the others follow it)
+// first: the token of the lane's numbers 0, 4, 8 and 12 (the others follow it).  Returns the scale's logarithm and its inverse.
 template <int NH, bool BF16>
-__device__ __forceinline__ int open_values(uint4 (&raw)[NH][2], int first, int n, h8 (&o)[NH][2]) {
+__device__ __forceinline__ float2 open_values(uint4 (&raw)[NH][2], int first, int n, h8 (&o)[NH][2]) {
   uint32_t keep[2];
 #pragma unroll
   for (int i = 0; i < 2; ++i) keep[i] = (first + 2 * i < n ? 0xffffu : 0u) | (first + 2 * i + 1 < n ? 0xffff0000u : 0u);
@@ -113,7 +119,13 @@ __device__ __forceinline__ int open_values(uint4 (&raw)[NH][2], int first, int n
       }
       raw[x][e] = uint4{wd[0], wd[1], wd[2], wd[3]};
     }
-  const float amax = elem_to_float<BF16>(wave_max(top));
+  top = wave_max(top);
+  const bool bad = top >= (BF16 ? 0x7f80u : 0x7c00u);
+  if (bad) {
+#pragma unroll
+    for (int x = 0; x < NH; ++x) raw[x][0] = raw[x][1] = uint4{0, 0, 0, 0};
+  }
+  const float amax = bad ? 0.f : elem_to_float<BF16>(top);
   int ex = amax > 0.f ? 6 - ilogbf(amax) : 0;
   ex = ex > 64 ? 64 : ex;
   const float up = ldexpf(1.0f, ex);
@@ -127,7 +139,7 @@ __device__ __forceinline__ int open_values(uint4 (&raw)[NH][2], int first, int n
         o[x][e][2 * i + 1] = (_Float16)(elem_to_float<BF16>(word(raw[x][e], i) >> 16) * up);
       }
     }
-  return ex;
+  return bad ? float2{NAN, 0.f} : float2{(float)-ex, up};
 }
 // Halves of a query row's 8 numbers, given in bfloat16 times a power of two.
 __device__ __forceinline__ h8 query_halves(const uint4& raw, float up) {
@@ -242,15 +254,15 @@ __device__ __forceinline__ Split split_all(const PagedView& V, const AttendArgs&
 // Four channels of output row `at` from the weighted values, the reference and the sum of the weights.
 template <int D, bool BF16>
 __device__ __forceinline__ void write_row(const PagedView& V, const AttendArgs& a, int64_t at, int ch, f4 o, float M, float sum) {
-  const float inv = sum > 0.f ? 1.0f / sum : 0.f;
+  const float inv = sum == 0.f ? 0.f : 1.0f / sum;      // (a NaN stays one)
   uint16_t u[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) u[i] = float_to_elem<BF16>(o[i] * inv);
   *reinterpret_cast<uint2*>(a.y + at * D + ch) = uint2{u[0] | (uint32_t)u[1] << 16, u[2] | (uint32_t)u[3] << 16};
-  if (ch == 0 && a.lse != nullptr) a.lse[at] = sum > 0.f ? (M + log2f(sum)) * 0.693147180559945309f : -INFINITY;
+  if (ch == 0 && a.lse != nullptr) a.lse[at] = sum == 0.f ? -INFINITY : (M + log2f(sum)) * 0.693147180559945309f;
 }
 
-struct Partial {          // of one item, KV head and row: reference, sum; the weighted values follow in another array
+struct Partial {          // of one piece or share, KV head and row: reference, sum; the weighted values are in another array
   float M, l;
 };
 
@@ -473,8 +485,8 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_rows_kernel(PagedView V, Att
 #pragma unroll
             for (int e = 0; e < 2; ++e) s[nt][0] = __builtin_amdgcn_mfma_f32_16x16x32_f16(o[x][e], q[nt][x][e], s[nt][0], 0, 0, 0);
         }
-        const int ex = open_values<NH, BF16>(raw[1], t0 + 4 * g, n, o);
-        const float lv = (float)-ex, iv = ldexpf(1.0f, ex);
+        const float2 vi = open_values<NH, BF16>(raw[1], t0 + 4 * g, n, o);
+        const float lv = vi.x, iv = vi.y;
         h2 p[NT][1][2];
         weigh(std::integral_constant<int, 1>{}, s, &ks, &lv, &iv, t0, n, p);
 #pragma unroll
@@ -490,7 +502,7 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_rows_kernel(PagedView V, Att
       }
     }
 
-    float sc_lv = log2_raw(sc.y), sc_iv = 1.0f / sc.y;
+    float sc_lv = log2_raw(sc.y), sc_iv = inverse_scale(sc.y);
     for (int k = 0; k < nk; ++k) {
       const int kg = k % group;
       if (kg == 0) next_id = ask_id(k + group);
@@ -524,7 +536,7 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_rows_kernel(PagedView V, Att
           id = next_id;
           sc = next_sc;
           sc_lv = log2_raw(sc.y);
-          sc_iv = 1.0f / sc.y;
+          sc_iv = inverse_scale(sc.y);
         }
         load(k + 1, kw, 0);
       }
@@ -886,7 +898,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void paged_tile_kernel(PagedV
     float ks = nks, lv, iv;
     if (nid >= 0) {
       lv = log2_raw(nvs);
-      iv = 1.0f / nvs;
+      iv = inverse_scale(nvs);
 #pragma unroll
       for (int z = 0; z < NH; ++z)
 #pragma unroll
@@ -918,7 +930,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void paged_tile_kernel(PagedV
       for (int z = 0; z < NH; ++z)
 #pragma unroll
         for (int e = 0; e < 2; ++e) put_key(buf, z, e, o[z][e]);
-      const int vx = open_values<NH, BF16>(raw[1], t + 4 * g, n, o);
+      const float2 vi = open_values<NH, BF16>(raw[1], t + 4 * g, n, o);
 #pragma unroll
       for (int z = 0; z < NH; ++z)
 #pragma unroll
@@ -928,8 +940,8 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void paged_tile_kernel(PagedV
           put_value(buf, z, 2 * e + 1, h2{v[4], v[5]}, h2{v[6], v[7]});
         }
       ks = ldexpf(1.0f, -kx);
-      lv = (float)-vx;
-      iv = ldexpf(1.0f, vx);
+      lv = vi.x;
+      iv = vi.y;
     } else {                                                     // no tokens: zeros, and no weight
       const h8 zero = {0, 0, 0, 0, 0, 0, 0, 0};
       const h2 none = {0, 0};
@@ -1042,7 +1054,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void paged_tile_kernel(PagedV
   }
   if (!live) return;
   const int64_t out = (int64_t)(row0 + qi) * V.hq + hq;
-  const float inv = l > 0.f ? 1.0f / l : 0.f;
+  const float inv = l == 0.f ? 0.f : 1.0f / l;
 #pragma unroll
   for (int c = 0; c < NC; ++c)
 #pragma unroll
@@ -1052,7 +1064,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void paged_tile_kernel(PagedV
       for (int x = 0; x < 4; ++x) o[x] = float_to_elem<BF16>(y[c][i + x] * inv);
       *reinterpret_cast<uint2*>(a.y + out * D + 32 * c + 8 * (i >> 2) + 4 * hh) = uint2{o[0] | (uint32_t)o[1] << 16, o[2] | (uint32_t)o[3] << 16};
     }
-  if (hh == 0 && a.lse != nullptr) a.lse[out] = l > 0.f ? (M + log2f(l)) * 0.693147180559945309f : -INFINITY;
+  if (hh == 0 && a.lse != nullptr) a.lse[out] = l == 0.f ? -INFINITY : (M + log2f(l)) * 0.693147180559945309f;
 }
 
 // Joins the shares of divided tiles: a group of D / 4 threads per query row and head, tp.join rows to a workgroup.

@@ -386,6 +386,52 @@ def test_attend_skips_pages_that_do_not_exist(B):
     assert bool((y[1] == 0).all()) and bool(torch.isinf(lse[1]).all())
 
 
+@pytest.mark.parametrize("D,elem,code", [(128, "f16", "int8"), (128, "bf16", "e4m3"), (64, "bf16", "int8"), (64, "f16", "e4m3")])
+@pytest.mark.parametrize("what", [math.nan, math.inf])
+@pytest.mark.parametrize("side", [0, 1])
+@pytest.mark.parametrize("m,n", [(3, 200), (100, 200), (4, 2100), (150, 2100)])
+def test_infinities_and_nan_reach_only_the_queries_that_see_their_block(B, D, elem, code, what, side, m, n):
+    """Sequence 0 has one in a whole block, sequence 1 in its open rows, both behind the first queries and in one KV head."""
+    P, hkv, G = 32, 2, 3
+    lens = [n, n + 20 - n % P]
+    rig = Rig(B, 2, hkv * G, hkv, D, P, elem, code, 2 * 70, 70, seed=n + m)
+    x = [rig.rows(sum(lens), hkv, D), rig.rows(sum(lens), hkv, D)]
+    # the last whole block of sequence 0, and the last token of sequence 1
+    at = [(n // P - 1) * P + 31 if m > 3 else n // P * P - 1, lens[1] - 1]
+    clean = [t.clone() for t in x]
+    x[side][at[0], 1, 7] = what
+    x[side][lens[0] + at[1], 1, 7] = what
+    rig.store(lens, k=x[0], v=x[1])
+    block = rig.tables[0][n // P - 1]
+    assert torch.isnan(rig.scale[block, 1, side]) and bool(torch.isfinite(rig.scale[block, 0]).all())
+    q = rig.rows(2 * m, hkv * G, D)
+    y, lse, ws = (torch.full((2 * m, hkv * G, D), -77.0, dtype=q.dtype, device="cuda"), torch.full((2 * m, hkv * G), -77.0, device="cuda"),
+                  torch.empty(B.hca_paged_workspace_bytes(rig.shape, 2 * m, m), dtype=torch.uint8, device="cuda"))
+    qd, sm = q.cuda(), 1.0 / math.sqrt(D)
+    B.hca_paged_attend(rig.shape, qd, qd.stride(0), dev([0, m, 2 * m]), 2 * m, m, dev(lens), n, dev(rig.tables), rig.kv, rig.scale,
+                       rig.open, sm, True, y, lse, ws)
+    torch.cuda.synchronize()
+    y, lse = y.cpu(), lse.cpu()
+    # the same without it: what the queries that do not see it are compared with
+    rig.ref.store([0, 0], [0, lens[0], sum(lens)], clean[0], clean[1], rig.tables)
+    for b in range(2):
+        k, v, there = rig.ref.read(b, lens[b], rig.tables)
+        rows = q[b * m:b * m + m]
+        ry, rl, mass, big = R.attend(rows, k, v, there, sm, True, G)
+        ty, tl = R.tolerances(ry, rl, mass, big, lens[b], D, elem)
+        # query i sees positions <= lens - m + i; the NaN reaches those that see the first token of its block / open tile
+        first = at[0] // P * P if b == 0 else lens[1] // 16 * 16
+        sees = torch.arange(m) + lens[b] - m
+        y0, l0 = y[b * m:b * m + m], lse[b * m:b * m + m]
+        ok = torch.ones(m, hkv * G, dtype=torch.bool)
+        ok[sees >= first, G:] = False
+        assert bool((((y0.double() - ry).abs() <= ty).all(-1) | ~ok).all())
+        assert bool((((l0.double() - rl).abs() <= tl) | ~ok).all())
+        if b == 0 or math.isnan(what) or side == 1:
+            hit = sees >= (first if b == 0 else at[1])
+            assert bool(torch.isnan(y0[hit, G:]).all()) and bool(torch.isnan(l0[hit, G:]).all())
+
+
 def test_attend_computes_no_more_queries_than_told(B):
     rig = filled(B, [100, 90], 4, 2, 128, 16, "f16", "e4m3", seed=7)
     q = rig.rows(9, 4, 128)
