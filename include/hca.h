@@ -602,8 +602,8 @@ int32_t hca_vq_evict(const hca_shape* shape, const hca_vq_codebook* cb, void* pc
  * kv, scale and open need no initial values; kv, open and rows of new keys, values and queries are 16-byte aligned, scale
  * is 8-byte aligned.
  * Supported: head_dim 64 or 128; page 16, 32, 64 or 128; n_q_heads / n_kv_heads 1 .. 16; up to 1024 sequences of up to 2^30
- * tokens, 2^37 in all rows of the table together; n_pages * page below 2^31; calls of up to 2^27 new rows and 2^22 query
- * rows (fewer where total_q * n_q_heads comes near 2^31).  Anything else: HCA_ERR_UNSUPPORTED. */
+ * tokens, 2^36 in all rows of the table together; n_pages * page below 2^31; calls of up to 2^27 new rows (of fewer than
+ * 2^23 blocks of one KV head in all) and 2^22 query rows (fewer where total_q * n_q_heads comes near 2^31).  Anything else: HCA_ERR_UNSUPPORTED. */
 #define HCA_F16 0      /* elem: IEEE half */
 #define HCA_BF16 1     /* elem: bfloat16 */
 #define HCA_INT8 0     /* code: signed integers -127 .. 127 */
@@ -641,6 +641,7 @@ size_t hca_paged_workspace_bytes(const hca_paged_shape* shape, int64_t total_q, 
  *   tok_seq, tok_pos, tok_slot   device, int32 [max_new] each, or NULL: sequence, position and slot (page * P + position
  *              % P) of every new token; -1 position and slot in a refused sequence; rows from cu[n_seqs] on are left
  *              as they were
+ * A page belongs to one row of the table: the call does not count how many rows name it.
  * Pages of ending sequences are pushed first (ascending sequence, ascending block), then pages are popped in the
  * same order, so a step can use what it frees.  A sequence is refused - its length and pages stay as they were -
  * if its length would pass max_pages * P, if its rows would pass max_new, or if it needs pages and the pages

@@ -12,7 +12,7 @@ int32_t paged_view(const hca_paged_shape* s, PagedView* V) {
   if (!(s->page == 16 || s->page == 32 || s->page == 64 || s->page == 128)) return HCA_ERR_UNSUPPORTED;
   if (!(s->elem == HCA_F16 || s->elem == HCA_BF16) || !(s->code == HCA_INT8 || s->code == HCA_E4M3)) return HCA_ERR_UNSUPPORTED;
   if ((int64_t)s->max_pages * s->page > (int64_t)1 << 30) return HCA_ERR_UNSUPPORTED;
-  if ((int64_t)s->n_seqs * s->max_pages > ((int64_t)1 << 37) / s->page) return HCA_ERR_UNSUPPORTED;   // tokens of all rows
+  if ((int64_t)s->n_seqs * s->max_pages > ((int64_t)1 << 36) / s->page) return HCA_ERR_UNSUPPORTED;   // tokens of all rows
   if (s->n_pages > INT32_MAX / s->page) return HCA_ERR_UNSUPPORTED;   // slots are int32
   V->n_seqs = s->n_seqs;
   V->hq = s->n_q_heads;

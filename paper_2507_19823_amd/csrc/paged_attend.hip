@@ -226,7 +226,7 @@ struct Split {
   bool shares;          // each sequence in equal shares of at most C units; else ranges of C units across sequences
   __device__ int count(int units) const { return shares ? (units + C - 1) / C : units; }     // what is numbered through
 };
-// All units together are fewer than 2^31 (see paged_view).  items(C): workgroups that shares of up to C units take.
+// All units together are at most 2^30 + 1024 (see paged_view).  items(C): workgroups that shares of up to C units take.
 template <typename F>
 __device__ __forceinline__ Split split_of(const SplitPlan& sp, uint32_t all, F&& items) {
   int C = (int)((all + (uint32_t)sp.want - 1) / (uint32_t)sp.want);

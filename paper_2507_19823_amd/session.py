@@ -110,6 +110,7 @@ class PagedCache:
         if nbytes == 0:
             raise B.HcaError("hca_paged_cache_bytes", -2)
         i32 = dict(dtype=torch.int32, device=device)
+        self.n_seqs, self.hq, self.hkv, self.head_dim = n_seqs, n_q_heads, n_kv_heads, head_dim
         self.dtype = {"f16": torch.float16, "bf16": torch.bfloat16}[elem]
         self.max_tokens, self.max_len = max_tokens, max_pages * page
         side = page * head_dim
@@ -126,20 +127,51 @@ class PagedCache:
         self.ws = torch.empty(B.hca_paged_workspace_bytes(self.shape, max_tokens, max_tokens), dtype=torch.uint8, device=device)
         self.sm_scale = 1.0 / math.sqrt(head_dim)
 
+    def _check(self, name, t, dtype, *shape, packed=True):
+        """t has what a call reads or writes by address: type, device, sizes, and its numbers where they are expected."""
+        strides, want = t.stride(), 1
+        inner = True
+        for n, st in zip(reversed(shape[1:]), reversed(strides[1:])):
+            inner, want = inner and (st == want or n == 1), want * n
+        if packed:
+            inner = inner and (not shape or shape[0] <= 1 or strides[0] == want)
+        if t.dtype != dtype or t.device != self.lens.device or tuple(t.shape) != shape or not inner:
+            raise ValueError(f"{name}: {tuple(t.shape)} {t.dtype} on {t.device}, strides {strides}; expected {shape} {dtype} on "
+                             f"{self.lens.device}" + (", contiguous" if packed else ", rows of contiguous heads"))
+
+    def _rows(self, name, n):
+        if n > self.max_tokens:
+            raise ValueError(f"{name}: {n} rows, made for max_tokens = {self.max_tokens}")
+        if self.lens.is_cuda and torch.cuda.current_device() != self.lens.device.index:
+            raise ValueError(f"{name}: the cache is on {self.lens.device}, which is not the current device")
+
     def step(self, add, total, stream=None):
         """add: device int32 [n_seqs], new tokens per sequence, negative where one ends; total: rows that the step's keys,
         values and queries have (>= the sum of the positive entries, <= max_tokens)."""
-        assert total <= self.max_tokens
+        self._rows("step", total)
+        self._check("add", add, torch.int32, self.n_seqs)
         B.hca_paged_map(self.shape, add, self.lens, self.lens, self.tables, self.free, self.n_free, self.n_free, total, self.start,
                         self.cu, self.tok[0], self.tok[1], self.tok[2], stream)
 
     def store(self, layer, k, v, stream=None):
         """k, v: [total, n_kv_heads, head_dim], rows as step() numbered them; slices of a fused projection will do."""
+        self._rows("k", k.shape[0])
+        self._check("k", k, self.dtype, k.shape[0], self.hkv, self.head_dim, packed=False)
+        self._check("v", v, self.dtype, k.shape[0], self.hkv, self.head_dim, packed=False)
         B.hca_paged_store(self.shape, k, k.stride(0), v, v.stride(0), k.shape[0], self.start, self.cu, self.tables,
                           self.kv[layer], self.scale[layer], self.open[layer], stream)
 
     def attend(self, layer, q, max_q, y, lse=None, causal=True, max_len=None, cu=None, stream=None):
-        """q: [total, n_q_heads, head_dim] -> y, for the step's own tokens; cu: row offsets of other queries (cross attention)."""
+        """q: [total, n_q_heads, head_dim] -> y, for the step's own tokens; cu: row offsets of other queries (cross attention),
+        max_tokens of them at most."""
+        total = q.shape[0]
+        self._rows("q", total)
+        self._check("q", q, self.dtype, total, self.hq, self.head_dim, packed=False)
+        self._check("y", y, self.dtype, total, self.hq, self.head_dim)
+        if lse is not None:
+            self._check("lse", lse, torch.float32, total, self.hq)
+        if cu is not None:
+            self._check("cu", cu, torch.int32, self.n_seqs + 1)
         B.hca_paged_attend(self.shape, q, q.stride(0), self.cu if cu is None else cu, q.shape[0], max_q, self.lens,
                            self.max_len if max_len is None else max_len, self.tables, self.kv[layer], self.scale[layer],
                            self.open[layer], self.sm_scale, causal, y, lse, self.ws, stream)

@@ -565,6 +565,39 @@ def test_captured_step_replayed_while_lengths_grow(B):
     run_steps(c, ref, tabs, steps, layers, hq, hkv, D, 12, call)
 
 
+@pytest.mark.parametrize("D,elem,code", [(128, "bf16", "e4m3"), (64, "f16", "int8")])
+def test_captured_chunk_replayed_at_other_lengths(B, D, elem, code):
+    """A graph of many query rows: whole tiles, divided ones and the join, at lengths that change between replays."""
+    hq, hkv, P, m = 8, 2, 64, 96
+    c, ref, tabs = make_pair(1, 2, hq, hkv, D, P, elem, code, 80, 60, 2 * m)
+    x = torch.zeros(2 * m, hq + 2 * hkv, D, dtype=c.dtype, device="cuda")
+    add, y, lse = dev([m, m]), torch.zeros(2 * m, hq, D, dtype=c.dtype, device="cuda"), torch.zeros(2 * m, hq, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        c.step(add, 2 * m)
+        c.store(0, x[:, hq:hq + hkv], x[:, hq + hkv:])
+        c.attend(0, x[:, :hq], m, y, lse)
+
+    def call(a, total, qkv):
+        add.copy_(dev(a))
+        x[:total].copy_(qkv[0])
+        graph.replay()
+        torch.cuda.synchronize()
+        _ = (x.float().sum() + 1).item()
+        return [y[:total]], [lse[:total]]
+
+    run_steps(c, ref, tabs, [[m, 5]] + [[m, m]] * 4 + [[1, m], [-1, 70], [m, 0]] + [[m, m]] * 2, 1, hq, hkv, D, 13, call)
+
+
+def test_cache_of_another_device_than_the_current_one(B, monkeypatch):
+    c, _, _ = make_pair(1, 2, 4, 2, 64, 16, "f16", "int8", 8, 4, 4)
+    x = torch.zeros(2, 8, 64, dtype=c.dtype, device="cuda")
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: c.lens.device.index + 1)
+    for call in (lambda: c.step(dev([1, 1]), 2), lambda: c.store(0, x[:, 4:6], x[:, 6:]), lambda: c.attend(0, x[:, :4], 1, x[:, :4].clone())):
+        with pytest.raises(ValueError, match="current device"):
+            call()
+
+
 def test_queries_over_an_encoders_states(B):
     """Cross attention: the states are stored once, the decoder's queries have another length and no mask."""
     hq, hkv, D = 6, 6, 64

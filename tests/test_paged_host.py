@@ -101,3 +101,36 @@ def test_attend_refuses(B):
     assert rc(total=2 ** 26 + 1) == -2 and rc(total=2 ** 22 + 1) == -2
     assert rc(scale=C.c_void_p(260)) == -1
     assert rc(total=0, q=None, y=None) == 0 and rc(max_q=0) == 0
+
+
+def test_paged_cache_checks_what_calls_take_by_address(B):
+    """Types, sizes, strides, devices and the rows that the workspace was made for, before anything is launched."""
+    import torch
+    from paper_2507_19823_amd.session import PagedCache
+    c = PagedCache(1, 3, 4, 2, 16, 10, 5, 64, "f16", "int8", max_tokens=8, device="cpu")
+    h = dict(dtype=torch.float16)
+    k, q, y, lse = torch.zeros(4, 2, 64, **h), torch.zeros(4, 4, 64, **h), torch.zeros(4, 4, 64, **h), torch.zeros(4, 4)
+    add = torch.ones(3, dtype=torch.int32)
+    for bad in (add.long(), add[:2], torch.ones(3, 2, dtype=torch.int32)[:, 0], add.to("meta")):
+        with pytest.raises(ValueError, match="add"):
+            c.step(bad, 3)
+    with pytest.raises(ValueError, match="max_tokens"):
+        c.step(add, 9)
+    wide = torch.zeros(4, 64, 2, **h)
+    for bad in (k.bfloat16(), k[:3], torch.zeros(4, 2, 128, **h), wide.transpose(1, 2), torch.zeros(4, 4, 64, **h)[:, ::2]):
+        with pytest.raises(ValueError, match="v:"):
+            c.store(0, k, bad)
+    with pytest.raises(ValueError, match="k:"):
+        c.store(0, wide.transpose(1, 2), k)
+    with pytest.raises(ValueError, match="max_tokens"):             # a workspace of single queries' size would be overrun
+        c.attend(0, torch.zeros(9, 4, 64, **h), 9, torch.zeros(9, 4, 64, **h))
+    with pytest.raises(ValueError, match="y:"):
+        c.attend(0, q, 1, torch.zeros(4, 8, 64, **h)[:, :4], lse)
+    with pytest.raises(ValueError, match="lse:"):
+        c.attend(0, q, 1, y, lse.double())
+    with pytest.raises(ValueError, match="cu:"):
+        c.attend(0, q, 1, y, lse, cu=torch.zeros(3, dtype=torch.int32))
+    with pytest.raises(ValueError, match="q:"):
+        c.attend(0, q[:, :2], 1, y, lse)
+    with pytest.raises(B.HcaError):
+        PagedCache(1, 3, 4, 2, 16, 10, 5, 80, device="cpu")
