@@ -1169,15 +1169,16 @@ static int32_t launch_rows(const PagedView& V, const AttendArgs& a, int64_t max_
   return wide ? launch_rows_nt<D, 2, 8>(V, a, sp, ws, st) : launch_rows_nt<D, 2, 4>(V, a, sp, ws, st);
 }
 
-// Whether a rest of tiles is divided.  The second launch and the partial results have a price, 5 us for a few tiles and 10 for many.
-// Where all tiles are fewer than the places: from 384 tokens on for very few (two times 40 rows over 500 tokens: 18.7 us
-// whole, 15.5 divided; over 300 tokens 14.0 and 15.5), from 768 on for more (a prompt of 700 tokens: 26.3 us whole, 30.3
-// divided; of 1000: 40 and 39).  Behind up to five whole rounds: where tiles are long and about equally long - that is not for
-// prompts from their first token on, whose short tiles fill the last round by themselves.
+// Whether a rest of tiles is divided.  Where all tiles are fewer than the places, in units of 64 tokens' time: whole tiles take as many as they
+// see, divided ones that times tiles / places, and a third more since workgroups then share compute units; the second launch and the
+// partial results cost 5.5 for a few tiles and up to 20 more for many.  Whole / divided, us: 2 x 40 rows over 300 tokens 14.0 /
+// 15.5, over 500 18.7 / 15.5; of 64 places 2 tiles of 900 tokens 32 / 20, 10 of up to 1158 36 / 33, 36 of up to 1158 40 / 49, 39 of
+// 1133 49 / 62, 29 of up to 1500 49 / 56, 24 of up to 2710 74 / 69.  Behind up to five whole rounds: where tiles are long and about equally
+// long - that is not for prompts from their first token on, whose short tiles fill the last round by themselves.
 static bool divides_tiles(const PagedView& V, const AttendArgs& a, int64_t max_len) {
-  const int64_t tiles = (int64_t)a.total * V.gqa / kTileRows;
-  if (tiles < rows_want(V)) return max_len > (16 * tiles < rows_want(V) ? 384 : 768);
-  return tiles < 6 * rows_want(V) && max_len >= 8192 && (!a.causal || max_len / 4 >= a.max_q);
+  const int64_t tiles = (int64_t)a.total * V.gqa / kTileRows, places = rows_want(V);
+  if (tiles < places) return max_len / kUnit * (100 * places - 135 * tiles) > 550 * places + 2000 * tiles;
+  return tiles < 6 * places && max_len >= 8192 && (!a.causal || max_len / 4 >= a.max_q);
 }
 
 template <int D>
@@ -1244,6 +1245,8 @@ int32_t hca_paged_attend(const hca_paged_shape* shape, const void* q, int64_t q_
   // a launch has fewer than 2^32 threads along x: 2^24 workgroups
   if (total_q > (int64_t)1 << 22 || total_q * V.hq / kTileRows + (int64_t)2048 * V.hkv >= (int64_t)1 << 24) return HCA_ERR_UNSUPPORTED;
   if (total_q == 0 || max_q == 0) return HCA_OK;
+  const int64_t room = (int64_t)V.max_pages << V.lp;
+  if (max_len > room) max_len = room;
   const AttendArgs a{(const uint16_t*)q, q_stride, cu, lens, tables, (const uint8_t*)kv, scale, (const uint16_t*)open,
                      sm_scale * 1.44269504088896341f, (int32_t)total_q, (int32_t)(max_q < total_q ? max_q : total_q), causal, (uint16_t*)y, lse};
   hipStream_t st = (hipStream_t)stream;
