@@ -196,7 +196,7 @@ __device__ __forceinline__ float largest(const uint4& raw) {
 constexpr int kUnit = 64;
 
 struct SplitPlan {
-  int32_t want;         // workgroups per KV head; 0: a workgroup per sequence, nothing to join
+  int32_t want;         // workgroups per KV head; 0: a workgroup per row of the table, nothing to join
   int32_t least;        // units per workgroup at least
 };
 
@@ -282,44 +282,48 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_rows_kernel(PagedView V, Att
   const int h = blockIdx.y, G = V.gqa;
   const int64_t side = V.side();
 
-  // the workgroup's piece: from unit u of sequence b on, `left` units.  Up to 64 sequences: their lengths are read once.
+  // the workgroup's piece: from unit u of sequence b on, `left` units.  Without division: row blockIdx.x of the table, no search (1000
+  // sequences of up to 40 tokens: 133 us with one, 71 so).  Up to 64 sequences: their lengths are read once.
   int b, u, left = 0;
   Seq sq;
   Split cut{1, false};
-  const auto numbered = [&](int units) { return sp.want == 0 ? (units > 0 ? 1 : 0) : cut.count(units); };
-  const auto range = [&](uint32_t all) {                        // of the numbering: false if there is nothing for this workgroup
-    const int64_t U0 = (int64_t)blockIdx.x * cut.C;
-    left = all - U0 < cut.C ? (int)(all - U0) : cut.C;
-    return U0 < all;
-  };
-  Seq mine{0, 0, 0, 0};
-  if (lane < V.n_seqs) mine = seq_info(V, a, lane);
-  if (sp.want != 0) {
+  if (sp.want == 0) {
+    b = blockIdx.x;
+    sq = seq_info(V, a, b);
+    if (sq.units == 0) return;
+    u = 0;
+    left = sq.units;
+  } else {
+    Seq mine{0, 0, 0, 0};
+    if (lane < V.n_seqs) mine = seq_info(V, a, lane);
     uint32_t all;
     cut = split_all(V, a, sp, mine, &all);
-    if (!cut.shares && !range(all)) return;
+    if (!cut.shares) {
+      const int64_t U0 = (int64_t)blockIdx.x * cut.C;
+      left = all - U0 < cut.C ? (int)(all - U0) : cut.C;
+      if (U0 >= all) return;
+    }
+    const int i = cut.shares ? (int)blockIdx.x : (int)blockIdx.x * cut.C;
+    if (V.n_seqs <= 64) {
+      const int c = cut.count(mine.units);
+      const uint32_t incl = wave_scan_incl((uint32_t)c);
+      const uint64_t past = __ballot(incl > (uint32_t)i);
+      if (past == 0) return;
+      const int l = __builtin_ctzll(past);
+      b = l;
+      u = i - (__builtin_amdgcn_readlane((int)incl, l) - __builtin_amdgcn_readlane(c, l));
+      sq = seq_of_lane(mine, l);
+    } else {
+      b = paged_find(V.n_seqs, i, &u, [&](int x) { return cut.count(seq_units(V, a, x)); });
+      if (b >= V.n_seqs) return;
+      sq = seq_info(V, a, b);
+    }
+    if (cut.shares) {
+      const int count = cut.count(sq.units), share = u;
+      u = (int)((int64_t)sq.units * share / count);
+      left = (int)((int64_t)sq.units * (share + 1) / count) - u;
+    }
   }
-  const int i = sp.want == 0 || cut.shares ? (int)blockIdx.x : (int)blockIdx.x * cut.C;
-  if (V.n_seqs <= 64) {
-    const int c = numbered(mine.units);
-    const uint32_t incl = wave_scan_incl((uint32_t)c);
-    const uint64_t past = __ballot(incl > (uint32_t)i);
-    if (past == 0) return;
-    const int l = __builtin_ctzll(past);
-    b = l;
-    u = i - (__builtin_amdgcn_readlane((int)incl, l) - __builtin_amdgcn_readlane(c, l));
-    sq = seq_of_lane(mine, l);
-  } else {
-    b = paged_find(V.n_seqs, i, &u, [&](int x) { return numbered(seq_units(V, a, x)); });
-    if (b >= V.n_seqs) return;
-    sq = seq_info(V, a, b);
-  }
-  if (cut.shares) {
-    const int count = cut.count(sq.units), share = u;
-    u = (int)((int64_t)sq.units * share / count);
-    left = (int)((int64_t)sq.units * (share + 1) / count) - u;
-  }
-  if (sp.want == 0) left = sq.units;
 
   for (bool first = true;; first = false) {
     const int units = sq.units;
@@ -614,16 +618,18 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_rows_kernel(PagedView V, Att
   }
 }
 
-// Joins the pieces of sequences that have several.  One workgroup per query row and head, pieces in a fixed order.  A few KB
-// of reading that wait for one another: lengths, then the pieces' references, sums and values at once (each group of threads
-// keeps a running reference of its own), then the output.
+// Joins the pieces of sequences that have several, in a fixed order.  A few KB of reading that wait for one another: lengths, then the pieces'
+// references, sums and values at once, then the output.  A workgroup per row and head, whose groups of threads take a piece
+// each; or, where pieces are few (`grouped`), a workgroup per row and KV head, whose groups take a head each with all of its
+// pieces (256 sequences of up to 1100 tokens, two queries: of 16 heads on one 54 us one way and 27 the other, of 32 heads on
+// eight 129 and 104).
 template <int D>
-__global__ __launch_bounds__(256) void paged_join_kernel(PagedView V, AttendArgs a, SplitPlan sp, int cols, const Partial* __restrict__ ml,
+__global__ __launch_bounds__(256) void paged_join_kernel(PagedView V, AttendArgs a, SplitPlan sp, int cols, int grouped, const Partial* __restrict__ ml,
                                                          const float* __restrict__ part) {
-  constexpr int TPR = D / 4, NG = 256 / TPR;            // groups of threads, each with every NG-th piece
+  constexpr int TPR = D / 4, NG = 256 / TPR;            // groups of threads, four channels a thread
   __shared__ f4 s_o[NG][TPR];
   __shared__ Partial s_ml[NG];
-  const int hq = blockIdx.y, h = hq / V.gqa, lane = threadIdx.x & 63, t = blockIdx.x;
+  const int h = grouped ? blockIdx.y : blockIdx.y / V.gqa, lane = threadIdx.x & 63, t = blockIdx.x;
   Seq mine{0, 0, 0, 0};
   if (lane < V.n_seqs) mine = seq_info(V, a, lane);
   uint32_t all;
@@ -647,33 +653,53 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedView V, AttendArgs
   const int C = cut.shares ? 1 : cut.C;
   const int i0 = S / C, count = (E - 1) / C - i0 + 1;                    // its workgroups
   if (count <= 1) return;
-  const int r = i * V.gqa + hq % V.gqa;
   const int grp = threadIdx.x / TPR, ch = threadIdx.x % TPR * 4;
   const int late = S > i0 * C ? 1 : 0;                                   // the first piece is not its workgroup's first
-  const auto at = [&](int k) { return ((2 * (int64_t)(i0 + k) + (k == 0 ? late : 0)) * V.hkv + h) * cols + r; };
-  float M = -1e30f, sum = 0.f;
-  f4 o = {0.f, 0.f, 0.f, 0.f};
-  for (int k0 = grp; k0 < count; k0 += 4 * NG) {
-    Partial p[4];
-    f4 v[4];
+  const auto at = [&](int k, int r) { return ((2 * (int64_t)(i0 + k) + (k == 0 ? late : 0)) * V.hkv + h) * cols + r; };
+  float M, sum;
+  f4 o;
+  // pieces k, k + step, ... of row r
+  const auto join = [&](int r, int k, int step) {
+    M = -1e30f;
+    sum = 0.f;
+    o = f4{0.f, 0.f, 0.f, 0.f};
+    for (int k0 = k; k0 < count; k0 += 4 * step) {
+      Partial p[4];
+      f4 v[4];
 #pragma unroll
-    for (int x = 0; x < 4; ++x) {
-      const int64_t z = at(k0 + x * NG < count ? k0 + x * NG : k0);
-      p[x] = ml[z];
-      v[x] = *reinterpret_cast<const f4*>(part + z * D + ch);
-      if (k0 + x * NG >= count) p[x] = Partial{-1e30f, 0.f}, v[x] = f4{0.f, 0.f, 0.f, 0.f};
-    }
-    const float next = fmaxf(fmaxf(M, fmaxf(p[0].M, p[1].M)), fmaxf(p[2].M, p[3].M)), f0 = exp2_raw(M - next);
-    sum *= f0;
-    o *= f0;
-    M = next;
+      for (int x = 0; x < 4; ++x) {
+        const int64_t z = at(k0 + x * step < count ? k0 + x * step : k0, r);
+        p[x] = ml[z];
+        v[x] = *reinterpret_cast<const f4*>(part + z * D + ch);
+        if (k0 + x * step >= count) p[x] = Partial{-1e30f, 0.f}, v[x] = f4{0.f, 0.f, 0.f, 0.f};
+      }
+      const float next = fmaxf(fmaxf(M, fmaxf(p[0].M, p[1].M)), fmaxf(p[2].M, p[3].M)), f0 = exp2_raw(M - next);
+      sum *= f0;
+      o *= f0;
+      M = next;
 #pragma unroll
-    for (int x = 0; x < 4; ++x) {
-      const float f = exp2_raw(p[x].M - M);
-      sum = fmaf(p[x].l, f, sum);
-      o += v[x] * f;
+      for (int x = 0; x < 4; ++x) {
+        const float f = exp2_raw(p[x].M - M);
+        sum = fmaf(p[x].l, f, sum);
+        o += v[x] * f;
+      }
     }
+  };
+  const auto write = [&](int hq) {
+    if (V.elem == HCA_BF16)
+      write_row<D, true>(V, a, (int64_t)t * V.hq + hq, ch, o, M, sum);
+    else
+      write_row<D, false>(V, a, (int64_t)t * V.hq + hq, ch, o, M, sum);
+  };
+  if (grouped) {
+    for (int g = grp; g < V.gqa; g += NG) {
+      join(i * V.gqa + g, 0, 1);
+      write(h * V.gqa + g);
+    }
+    return;
   }
+  const int hq = blockIdx.y;
+  join(i * V.gqa + hq % V.gqa, grp, NG);
   s_o[grp][ch / 4] = o;
   if (ch == 0) s_ml[grp] = Partial{M, sum};
   __syncthreads();
@@ -687,10 +713,7 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedView V, AttendArgs
     sum = fmaf(s_ml[x].l, f, sum);
     o += s_o[x][ch / 4] * f;
   }
-  if (V.elem == HCA_BF16)
-    write_row<D, true>(V, a, (int64_t)t * V.hq + hq, ch, o, M, sum);
-  else
-    write_row<D, false>(V, a, (int64_t)t * V.hq + hq, ch, o, M, sum);
+  write(hq);
 }
 
 // ---- many query rows: the matrix cores are the bound -------------------------------------------------
@@ -1143,7 +1166,7 @@ static int32_t launch_rows_nt(const PagedView& V, const AttendArgs& a, const Spl
   const int64_t rows = 2 * (int64_t)rows_want(V) * V.hkv * 16 * NT;
   Partial* ml = (Partial*)ws;
   float* part = (float*)((char*)ws + align_up(rows * (int64_t)sizeof(Partial), 256));
-  const dim3 grid((unsigned)(sp.want == 0 ? (a.total < V.n_seqs ? a.total : V.n_seqs) : sp.want), (unsigned)V.hkv);
+  const dim3 grid((unsigned)(sp.want == 0 ? V.n_seqs : sp.want), (unsigned)V.hkv);
   const int which = (V.elem == HCA_BF16 ? 2 : 0) + (V.code == HCA_E4M3 ? 1 : 0);
   const auto kernel = which == 0 ? paged_rows_kernel<D, NT, NW, false, false> : which == 1 ? paged_rows_kernel<D, NT, NW, false, true>
                     : which == 2 ? paged_rows_kernel<D, NT, NW, true, false> : paged_rows_kernel<D, NT, NW, true, true>;
@@ -1155,7 +1178,9 @@ static int32_t launch_rows_nt(const PagedView& V, const AttendArgs& a, const Spl
   kernel<<<grid, 64 * NW, lds, st>>>(V, a, sp, ml, part);
   HCA_HIP(hipGetLastError());
   if (sp.want != 0) {
-    paged_join_kernel<D><<<dim3((unsigned)a.total, (unsigned)V.hq), 256, 0, st>>>(V, a, sp, 16 * NT, ml, part);
+    // up to about eight pieces per sequence (with 32 of them a group's walk is the longer one: 2 x 20000 tokens 29 and 33 us)
+    const int grouped = V.gqa > 1 && sp.want <= 8 * (int64_t)(a.total / a.max_q) ? 1 : 0;
+    paged_join_kernel<D><<<dim3((unsigned)a.total, (unsigned)(grouped ? V.hkv : V.hq)), 256, 0, st>>>(V, a, sp, 16 * NT, grouped, ml, part);
     HCA_HIP(hipGetLastError());
   }
   return HCA_OK;
