@@ -205,14 +205,7 @@ __device__ __forceinline__ int seq_len(const PagedView& V, const AttendArgs& a, 
   const int n = a.lens[b], most = V.max_pages << V.lp;
   return n < 0 ? 0 : n > most ? most : n;
 }
-// units of whole pages of sequence b: at least one if it has queries
-__device__ __forceinline__ int seq_units(const PagedView& V, const AttendArgs& a, int b) {
-  int f;
-  if (paged_rows(a.cu, b, a.total, &f) == 0) return 0;
-  const int u = ((seq_len(V, a, b) >> V.lp << V.lp) + kUnit - 1) / kUnit;
-  return u > 1 ? u : 1;
-}
-struct Seq { int row0, m, n, units; };                 // first query row, queries, tokens, units
+struct Seq { int row0, m, n, units; };                 // first query row, queries, tokens, units of whole pages: at least one if it has queries
 __device__ __forceinline__ Seq seq_info(const PagedView& V, const AttendArgs& a, int b) {
   Seq s;
   s.n = seq_len(V, a, b);
@@ -225,11 +218,42 @@ __device__ __forceinline__ Seq seq_of_lane(const Seq& s, int l) {
   return Seq{__builtin_amdgcn_readlane(s.row0, l), __builtin_amdgcn_readlane(s.m, l), __builtin_amdgcn_readlane(s.n, l),
              __builtin_amdgcn_readlane(s.units, l)};
 }
+// More than 64 sequences, 64 c + lane in s[c]: read at once, not 64 after 64 and again in every step of a division.  (Up to 64 have
+// a path of their own, 0.5 to 1 us shorter.)
+constexpr int kSeqChunks = kPagedMaxSeqs / 64;
+struct Seqs {
+  Seq s[kSeqChunks];
+  int chunks;
+  template <typename F> __device__ __forceinline__ void each(F&& f) const {
+#pragma unroll
+    for (int c = 0; c < kSeqChunks; ++c)
+      if (c < chunks) f(c, s[c]);
+  }
+};
+__device__ __forceinline__ Seqs seqs_of(const PagedView& V, const AttendArgs& a, const Seq& first) {
+  Seqs r;
+  r.chunks = (V.n_seqs + 63) / 64;
+  r.s[0] = first;
+  const auto load = [&](auto from, auto to) {
+#pragma unroll
+    for (int c = from; c < to; ++c) {
+      const int b = 64 * c + (threadIdx.x & 63);
+      r.s[c] = seq_info(V, a, b < V.n_seqs ? b : 0);
+      if (b >= V.n_seqs) r.s[c] = Seq{0, 0, 0, 0};
+    }
+  };
+  load(std::integral_constant<int, 1>{}, std::integral_constant<int, 4>{});
+#pragma unroll
+  for (int c = 4; c < kSeqChunks; ++c) r.s[c] = Seq{0, 0, 0, 0};
+  if (r.chunks > 4) load(std::integral_constant<int, 4>{}, std::integral_constant<int, kSeqChunks>{});
+  return r;
+}
 constexpr int kShort = 32;
 struct Split {
   int C;                // units per workgroup at most
   bool shares;          // each sequence in equal shares of at most C units; else ranges of C units across sequences
-  __device__ int count(int units) const { return shares ? (units + C - 1) / C : units; }     // what is numbered through
+  // what is numbered through (the quotient of a number up to 768 * 36 and one up to 36, half a step off: the rounding does not reach it)
+  __device__ int count(int units) const { return shares ? (int)(((float)(units + C) - 0.5f) * (1.0f / (float)C)) : units; }
 };
 // All units together are at most 2^30 + 1024 (see paged_view).  items(C): workgroups that shares of up to C units take.
 template <typename F>
@@ -241,19 +265,22 @@ __device__ __forceinline__ Split split_of(const SplitPlan& sp, uint32_t all, F&&
       if (items(x) <= (uint32_t)sp.want) return Split{x, true};
   return Split{C, false};
 }
-// mine: sequence `lane`, which callers have read already
-__device__ __forceinline__ Split split_all(const PagedView& V, const AttendArgs& a, const SplitPlan& sp, const Seq& mine, uint32_t* all) {
-  const auto sum = [&](auto&& f) {
-    uint32_t x = (uint32_t)f(mine.units);
-    for (int b = 64 + (threadIdx.x & 63); b < V.n_seqs; b += 64) x += (uint32_t)f(seq_units(V, a, b));
-    return wave_sum(x);
-  };
-  *all = sum([](int u) { return u; });
-  if (__popcll(__ballot(mine.units > 0)) <= 1 && V.n_seqs <= 64) {       // one sequence: ranges are shares
+__device__ __forceinline__ Split split_64(const SplitPlan& sp, const Seq& mine, uint32_t* all) {
+  *all = wave_sum((uint32_t)mine.units);
+  if (__popcll(__ballot(mine.units > 0)) <= 1) {       // one sequence: ranges are shares
     const int C = (int)((*all + (uint32_t)sp.want - 1) / (uint32_t)sp.want);
     return Split{C > sp.least ? C : sp.least, false};
   }
-  return split_of(sp, *all, [&](int C) { return sum([&](int u) { return (u + C - 1) / C; }); });
+  return split_of(sp, *all, [&](int C) { return wave_sum((uint32_t)((mine.units + C - 1) / C)); });
+}
+__device__ __forceinline__ Split split_many(const SplitPlan& sp, const Seqs& seqs, uint32_t* all) {
+  const auto sum = [&](auto&& f) {
+    uint32_t x = 0;
+    seqs.each([&](int, const Seq& s) { x += (uint32_t)f(s.units); });
+    return wave_sum(x);
+  };
+  *all = sum([](int u) { return u; });
+  return split_of(sp, *all, [&](int C) { return sum([&](int u) { return Split{C, true}.count(u); }); });
 }
 
 // Four channels of output row `at` from the weighted values, the reference and the sum of the weights.
@@ -296,28 +323,36 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_rows_kernel(PagedView V, Att
   } else {
     Seq mine{0, 0, 0, 0};
     if (lane < V.n_seqs) mine = seq_info(V, a, lane);
-    uint32_t all;
-    cut = split_all(V, a, sp, mine, &all);
-    if (!cut.shares) {
-      const int64_t U0 = (int64_t)blockIdx.x * cut.C;
-      left = all - U0 < cut.C ? (int)(all - U0) : cut.C;
-      if (U0 >= all) return;
-    }
-    const int i = cut.shares ? (int)blockIdx.x : (int)blockIdx.x * cut.C;
+    uint32_t all, before = 0;
+    int64_t i;                                          // the workgroup's first number
+    b = -1;
+    const auto find = [&](int c, const Seq& s) {
+      if (b >= 0) return;
+      const uint32_t n = (uint32_t)cut.count(s.units), incl = before + wave_scan_incl(n);
+      const uint64_t past = __ballot((int64_t)incl > i);
+      if (past != 0) {
+        const int l = __builtin_ctzll(past);
+        b = 64 * c + l;
+        u = (int)i - (__builtin_amdgcn_readlane((int)incl, l) - __builtin_amdgcn_readlane((int)n, l));
+        sq = seq_of_lane(s, l);
+      }
+      before = wave_last(incl);
+    };
+    const auto place = [&]() {
+      i = cut.shares ? blockIdx.x : (int64_t)blockIdx.x * cut.C;
+      left = all - i < cut.C ? (int)(all - i) : cut.C;
+    };
     if (V.n_seqs <= 64) {
-      const int c = cut.count(mine.units);
-      const uint32_t incl = wave_scan_incl((uint32_t)c);
-      const uint64_t past = __ballot(incl > (uint32_t)i);
-      if (past == 0) return;
-      const int l = __builtin_ctzll(past);
-      b = l;
-      u = i - (__builtin_amdgcn_readlane((int)incl, l) - __builtin_amdgcn_readlane(c, l));
-      sq = seq_of_lane(mine, l);
+      cut = split_64(sp, mine, &all);
+      place();
+      find(0, mine);
     } else {
-      b = paged_find(V.n_seqs, i, &u, [&](int x) { return cut.count(seq_units(V, a, x)); });
-      if (b >= V.n_seqs) return;
-      sq = seq_info(V, a, b);
+      const Seqs seqs = seqs_of(V, a, mine);
+      cut = split_many(sp, seqs, &all);
+      place();
+      seqs.each(find);
     }
+    if (b < 0) return;
     if (cut.shares) {
       const int count = cut.count(sq.units), share = u;
       u = (int)((int64_t)sq.units * share / count);
@@ -633,21 +668,29 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedView V, AttendArgs
   Seq mine{0, 0, 0, 0};
   if (lane < V.n_seqs) mine = seq_info(V, a, lane);
   uint32_t all;
-  const Split cut = split_all(V, a, sp, mine, &all);
+  Split cut;
   // the row's sequence b, query i, and the numbers before and up to it
   int b = -1, i = 0, S = 0, E = 0, before = 0;
-  for (int b0 = 0; b0 < V.n_seqs && b < 0; b0 += 64) {
-    if (b0 > 0) mine = b0 + lane < V.n_seqs ? seq_info(V, a, b0 + lane) : Seq{0, 0, 0, 0};
-    const uint32_t c = (uint32_t)cut.count(mine.units), incl = wave_scan_incl(c);
-    const uint64_t past = __ballot(mine.m > 0 && t >= mine.row0 && t < mine.row0 + mine.m);
+  const auto find = [&](int c, const Seq& s) {
+    if (b >= 0) return;
+    const uint32_t n = (uint32_t)cut.count(s.units), incl = wave_scan_incl(n);
+    const uint64_t past = __ballot(s.m > 0 && t >= s.row0 && t < s.row0 + s.m);
     if (past != 0) {
       const int l = __builtin_ctzll(past);
-      b = b0 + l;
-      i = t - __builtin_amdgcn_readlane(mine.row0, l);
+      b = 64 * c + l;
+      i = t - __builtin_amdgcn_readlane(s.row0, l);
       E = before + __builtin_amdgcn_readlane((int)incl, l);
-      S = E - __builtin_amdgcn_readlane((int)c, l);
+      S = E - __builtin_amdgcn_readlane((int)n, l);
     }
     before += (int)wave_last(incl);
+  };
+  if (V.n_seqs <= 64) {
+    cut = split_64(sp, mine, &all);
+    find(0, mine);
+  } else {
+    const Seqs seqs = seqs_of(V, a, mine);
+    cut = split_many(sp, seqs, &all);
+    seqs.each(find);
   }
   if (b < 0 || i >= a.max_q) return;
   const int C = cut.shares ? 1 : cut.C;
