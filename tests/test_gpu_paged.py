@@ -291,6 +291,20 @@ def test_attend_ranges_across_many_sequences(B, q, hq):
     rig.attend(rig.rows(cu[-1], hq, 64), cu, max_q=q, max_len=1 << 20)
 
 
+@pytest.mark.parametrize("n_seqs,hq,q,max_len", [(257, 4, 1, 1 << 20), (1024, 2, 1, 1 << 20), (600, 16, 2, 5000), (1024, 1, 3, 500),
+                                                 (300, 16, 4, 9000)])
+def test_attend_hundreds_of_sequences(B, n_seqs, hq, q, max_len):
+    """Idle rows of the table between the others, lengths from nothing to several pages, a long one near the end."""
+    lens = [0 if i % 5 == 2 else (53 * i) % 201 for i in range(n_seqs)]
+    lens[-3] = 480 if max_len <= 500 else 2500
+    rig = filled(B, lens, hq, 1, 64, 128, "f16", "e4m3", seed=n_seqs + q)
+    m = [0 if i % 3 == 1 and i != n_seqs - 3 else 1 + i % q for i in range(n_seqs)]
+    cu = [0]
+    for t in m:
+        cu.append(cu[-1] + t)
+    rig.attend(rig.rows(cu[-1], hq, 64), cu, max_q=q, max_len=max_len)
+
+
 @pytest.mark.parametrize("n_seqs,hkv,D,q", [(20, 128, 64, 1), (90, 64, 128, 1), (70, 128, 64, 3), (9, 256, 128, 2)])
 def test_attend_few_ranges_over_many_sequences(B, n_seqs, hkv, D, q):
     """So many KV heads that there are two to eight ranges per head: each spans sequences, whole ones among them."""
@@ -374,6 +388,17 @@ def test_attend_pages_of_very_different_scales(B):
     k[64:80], v[64:80] = 0.0, 0.0
     rig.store([n], k=k, v=v)
     rig.attend(rig.rows(1, 4, 128), [0, 1])
+
+
+@pytest.mark.parametrize("m", [1, 5, 90])
+@pytest.mark.parametrize("n", [200, 2300])
+def test_attend_pages_shared_between_sequences_and_rows_before_the_first(B, m, n):
+    """A common beginning held once, one page twice in a row of the table; the first sequence's queries are not row 0."""
+    rig = filled(B, [n, n - 37, n // 2], 8, 2, 128, 32, "bf16", "int8", seed=m)
+    rig.tables[1][:3] = rig.tables[0][:3]
+    rig.tables[2][1] = rig.tables[2][0] = rig.tables[0][2]
+    y, lse = rig.attend(rig.rows(4 + 3 * m, 8, 128), [4, 4 + m, 4 + 2 * m, 4 + 3 * m], max_len=1 << 20)
+    assert bool((y[:4] == -77.0).all()) and bool((lse[:4] == -77.0).all())
 
 
 def test_attend_skips_pages_that_do_not_exist(B):
